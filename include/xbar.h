@@ -376,6 +376,77 @@ int xbar_shortcut_bwd(const float* dy, float* dx, int batch, int h, int w, int c
 int xbar_absmax(const float* x, size_t n, float* result, void* ws, size_t ws_bytes, void* hip_stream);
 
 /*
+ * Group normalisation with an activation, channels last: the normalisation of a network that answers single requests or trains
+ * on small batches (no statistics over the batch).  x[batch][positions][channels]; groups of channels / groups neighbouring
+ * channels (groups divides channels).
+ *   gn_fwd   z = gamma (x - mean) invstd + beta (+ skip), y = act(z); mean and invstd = 1 / sqrt(var + eps) (biased variance)
+ *            [batch][groups] per sample and group, rounded to float before they are used, kept for gn_bwd
+ *   gn_bwd   error behind the activation g = act'(z) dy, z evaluated again from x, mean, invstd, gamma, beta (and skip: pass what the
+ *            forward pass had); dx, dgamma = sum g xhat, dbeta = sum g over batch and positions, dskip = g (NULL: not wanted; only
+ *            with skip)
+ *   act      XBAR_ACT_*; a ReLU's output and gradient are 0 where z is not above 0 (NaN too), as in relu_fwd
+ * skip (shape of x) may be NULL.  Outputs must not overlap inputs (XBAR_EINVAL for y, dx and dskip).  Statistics are accumulated in
+ * double precision in a fixed order.  ws: xbar_gn_workspace_bytes; channels <= 2^20, batch groups < 2^25, else XBAR_ESHAPE.
+ */
+#define XBAR_ACT_NONE 0
+#define XBAR_ACT_RELU 1
+#define XBAR_ACT_SILU 2   /* z / (1 + exp(-z)) */
+size_t xbar_gn_workspace_bytes(int batch, int positions, int channels, int groups);
+int xbar_gn_fwd(const float* x, const float* gamma, const float* beta, const float* skip, float* y, float* mean, float* invstd, int batch,
+                int positions, int channels, int groups, float eps, int act, void* ws, size_t ws_bytes, void* hip_stream);
+int xbar_gn_bwd(const float* x, const float* dy, const float* gamma, const float* beta, const float* skip, const float* mean,
+                const float* invstd, float* dx, float* dgamma, float* dbeta, float* dskip, int batch, int positions, int channels, int groups,
+                int act, void* ws, size_t ws_bytes, void* hip_stream);
+
+/*
+ * Low-rank adapters beside a projection whose devices stay as they are programmed: every row of the batch belongs to a request with an
+ * adapter of its own, and gets that adapter's digital correction on top of the shared projection (xbar_fwd) -- or on top of the error
+ * that comes back through it (xbar_bwd).  Adapter a holds A[a][rank][K] and B[a][rank][N], both of type XBAR_F32 or XBAR_BF16 (bfloat16),
+ * and scale[a] (float); the weight it adds is dW[k][n] = scale[a] sum_r A[a][r][k] B[a][r][n].
+ *   adapter_plan  sorts the rows of a batch by adapter: rows[M] int32, any order; a number outside [0, adapters) is a row without an
+ *                 adapter.  One plan serves all layers and both directions of the batch.  plan: xbar_adapter_plan_bytes(M, adapters)
+ *   adapter_fwd   T[m][r] = sum_k X[m][k] A[a][r][k] (kept for adapter_bwd; NULL: not wanted), Y[m][n] = base[m][n] + sum_r scale[a] T[m][r]
+ *                 B[a][r][n], a = rows[m].  Y may be base itself (in place).  Rows without an adapter: Y = base, T = 0
+ *   adapter_bwd   dT[m][r] = scale[a] sum_n dY[m][n] B[a][r][n]; dX[m][k] = base[m][k] + sum_r dT[m][r] A[a][r][k] (dX may be base itself; NULL:
+ *                 not wanted, base is not read); dA[a][r][k] = sum_m dT[m][r] X[m][k], dB[a][r][n] = scale[a] sum_m T[m][r] dY[m][n] over the rows
+ *                 of adapter a (zero where it has none), float whatever the adapters' type
+ * Products and sums in single precision, in a fixed order.  Other overlaps of outputs with inputs: XBAR_EINVAL.  A plan made for another
+ * M or number of adapters: nothing is written.  rank <= 128, adapters <= 65536, M <= 2^24, K and N < 2^24, M max(K, N) < 2^38, else XBAR_ESHAPE.
+ * ws: xbar_adapter_workspace_bytes(XBAR_OP_FWD or XBAR_OP_BWD, ...).
+ */
+#define XBAR_F32  0
+#define XBAR_BF16 1
+size_t xbar_adapter_plan_bytes(int M, int adapters);
+int xbar_adapter_plan(const int32_t* rows, int M, int adapters, void* plan, size_t plan_bytes, void* hip_stream);
+size_t xbar_adapter_workspace_bytes(int op, int M, int K, int N, int rank, int adapters);
+int xbar_adapter_fwd(const void* plan, size_t plan_bytes, const float* base, const float* X, const void* A, const void* B, int type,
+                     const float* scale, float* Y, float* T, int M, int K, int N, int rank, int adapters, void* ws, size_t ws_bytes,
+                     void* hip_stream);
+int xbar_adapter_bwd(const void* plan, size_t plan_bytes, const float* base, const float* dY, const float* X, const float* T, const void* A,
+                     const void* B, int type, const float* scale, float* dX, float* dA, float* dB, int M, int K, int N, int rank, int adapters,
+                     void* ws, size_t ws_bytes, void* hip_stream);
+
+/*
+ * Global norm of the gradients of many tensors, clipping by it, and the clipped SGD step (the step of all digital parameters at
+ * once).  grads, params, sizes: HOST arrays of `tensors` device addresses and element counts, read during the call only (a captured graph
+ * keeps the addresses); tensors of 0 elements are allowed and their addresses not looked at.
+ *   grad_norm  norm[0] = sqrt(sum over all tensors of g^2)
+ *   grad_clip  the same norm (of the gradients before), then g <- c g, c = max_norm / norm where norm > max_norm, else 1
+ *   clip_sgd   the same norm, then p <- p - lr (c g) with the bits of grad_clip and sgd, but the gradients stay as they are.
+ *              max_norm = INFINITY: c is 1
+ * The squares are summed in double precision in a fixed order; norm is rounded to float at the end.  Where a gradient is infinite or NaN the
+ * norm says so and nothing else is written.  What is written (the gradients of grad_clip, the parameters of clip_sgd, norm, ws) must
+ * not overlap itself or anything that is read: XBAR_EINVAL.  ws: xbar_grads_workspace_bytes(tensors).
+ */
+#define XBAR_GRADS_MAX_TENSORS 2048
+size_t xbar_grads_workspace_bytes(int tensors);
+int xbar_grad_norm(const float* const* grads, const size_t* sizes, int tensors, float* norm, void* ws, size_t ws_bytes, void* hip_stream);
+int xbar_grad_clip(float* const* grads, const size_t* sizes, int tensors, float max_norm, float* norm, void* ws, size_t ws_bytes,
+                   void* hip_stream);
+int xbar_clip_sgd(float* const* params, const float* const* grads, const size_t* sizes, int tensors, float lr, float max_norm, float* norm,
+                  void* ws, size_t ws_bytes, void* hip_stream);
+
+/*
  * ADC range statistics (Sec. IV-B: the maximum current through the ADCs is data dependent and comes
  * from output distribution statistics).  Runs the input stage and the contraction of xbar_fwd
  * (op = XBAR_OP_FWD: in = X[M][K]) or xbar_bwd (XBAR_OP_BWD: in = dY[M][N]) and, instead of

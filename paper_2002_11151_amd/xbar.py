@@ -15,6 +15,8 @@ LIB_PATH = os.path.join(HERE, "libxbar.so")
  ADC_PER_ARRAY, INPUT_OFFSET, PULSE_CODED) = (1, 2, 4, 8, 16, 32, 64, 128, 256, 512, 1024, 2048)
 PULSE_MAGNITUDE = 4096
 OP_FWD, OP_BWD, OP_UPDATE, OP_FCM, OP_UPDATE_PULSED = 0, 1, 2, 3, 4
+ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
+F32, BF16 = 0, 1
 ABI_VERSION = 2
 
 
@@ -135,6 +137,21 @@ _SIGNATURES = {
     "xbar_maxpool_bwd": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(ConvGeom), C.c_void_p]),
     "xbar_softmax_xent": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_float,
                                     C.c_void_p]),
+    "xbar_gn_workspace_bytes": (C.c_size_t, [C.c_int] * 4),
+    "xbar_gn_fwd": (C.c_int, [C.c_void_p] * 7 + [C.c_int] * 4 + [C.c_float, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "xbar_gn_bwd": (C.c_int, [C.c_void_p] * 11 + [C.c_int] * 5 + [C.c_void_p, C.c_size_t, C.c_void_p]),
+    "xbar_adapter_plan_bytes": (C.c_size_t, [C.c_int] * 2),
+    "xbar_adapter_plan": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "xbar_adapter_workspace_bytes": (C.c_size_t, [C.c_int] * 6),
+    "xbar_adapter_fwd": (C.c_int, [C.c_void_p, C.c_size_t] + [C.c_void_p] * 4 + [C.c_int] + [C.c_void_p] * 3 + [C.c_int] * 5 +
+                         [C.c_void_p, C.c_size_t, C.c_void_p]),
+    "xbar_adapter_bwd": (C.c_int, [C.c_void_p, C.c_size_t] + [C.c_void_p] * 6 + [C.c_int] + [C.c_void_p] * 4 + [C.c_int] * 5 +
+                         [C.c_void_p, C.c_size_t, C.c_void_p]),
+    "xbar_grads_workspace_bytes": (C.c_size_t, [C.c_int]),
+    "xbar_grad_norm": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "xbar_grad_clip": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_float, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "xbar_clip_sgd": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_float, C.c_float, C.c_void_p, C.c_void_p, C.c_size_t,
+                                C.c_void_p]),
     "xbar_shortcut_fwd": (C.c_int, [C.c_void_p, C.c_void_p] + [C.c_int] * 6 + [C.c_void_p]),
     "xbar_shortcut_bwd": (C.c_int, [C.c_void_p, C.c_void_p] + [C.c_int] * 6 + [C.c_void_p]),
     "xbar_absmax": (C.c_int, [C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
@@ -608,6 +625,176 @@ def absmax(x, ws=None):
     res = torch.empty(4, dtype=torch.float32, device=x.device)
     _check(lib().xbar_absmax(_dev(x), x.numel(), _dev(res), ws.data_ptr(), ws.numel(), _stream()))
     return float(res[0].item())
+
+
+def _here(*tensors):
+    """The library launches on the current device: its tensors have to lie there."""
+    device = torch.cuda.current_device()
+    assert all(t is None or t.get_device() == device for t in tensors), "a tensor is not on the current device"
+
+
+def _gn_ws(batch, positions, channels, groups, ws, device):
+    def size():
+        nbytes = lib().xbar_gn_workspace_bytes(batch, positions, channels, groups)
+        _check(0 if nbytes else -2)
+        return nbytes
+    return _buffer(size, ws, device)
+
+
+def gn_fwd(x, gamma, beta, groups, eps=1e-5, act=ACT_NONE, skip=None, ws=None):
+    """xbar_gn_fwd on x[batch][...][channels]: act(gn(x) + skip) as (y, mean, invstd), the statistics [batch][groups]."""
+    batch, channels = x.shape[0], x.shape[-1]
+    assert x.dim() >= 2 and x.numel() and gamma.shape == (channels,) == beta.shape and (skip is None or skip.shape == x.shape)
+    _here(x, gamma, beta, skip, ws)
+    positions = x.numel() // (batch * channels)
+    ws = _gn_ws(batch, positions, channels, groups, ws, x.device)
+    y = torch.empty_like(x)
+    mean = torch.empty((batch, groups), dtype=torch.float32, device=x.device)
+    invstd = torch.empty_like(mean)
+    _check(lib().xbar_gn_fwd(_dev(x), _dev(gamma), _dev(beta), None if skip is None else _dev(skip), _dev(y), _dev(mean), _dev(invstd), batch,
+                             positions, channels, groups, eps, act, ws.data_ptr(), ws.numel(), _stream()))
+    return y, mean, invstd
+
+
+def gn_bwd(x, dy, gamma, beta, mean, invstd, act=ACT_NONE, skip=None, ws=None):
+    """xbar_gn_bwd: returns (dx, dgamma, dbeta), with a skip (dx, dgamma, dbeta, dskip)."""
+    batch, channels = x.shape[0], x.shape[-1]
+    groups = mean.shape[-1]
+    assert x.dim() >= 2 and x.numel() and dy.shape == x.shape and gamma.shape == (channels,) == beta.shape
+    assert mean.shape == (batch, groups) == invstd.shape and (skip is None or skip.shape == x.shape)
+    _here(x, dy, gamma, beta, mean, invstd, skip, ws)
+    positions = x.numel() // (batch * channels)
+    ws = _gn_ws(batch, positions, channels, groups, ws, x.device)
+    dx = torch.empty_like(x)
+    dgamma = torch.empty(channels, dtype=torch.float32, device=x.device)
+    dbeta = torch.empty_like(dgamma)
+    dskip = None if skip is None else torch.empty_like(x)
+    _check(lib().xbar_gn_bwd(_dev(x), _dev(dy), _dev(gamma), _dev(beta), None if skip is None else _dev(skip), _dev(mean), _dev(invstd), _dev(dx),
+                             _dev(dgamma), _dev(dbeta), None if skip is None else _dev(dskip), batch, positions, channels, groups, act,
+                             ws.data_ptr(), ws.numel(), _stream()))
+    return (dx, dgamma, dbeta) if skip is None else (dx, dgamma, dbeta, dskip)
+
+
+class AdapterPlan:
+    """Rows of a batch in the order of their adapters, for all layers and both directions of that batch."""
+    __slots__ = ("buffer", "rows", "adapters")
+
+    def __init__(self, buffer, rows, adapters):
+        self.buffer, self.rows, self.adapters = buffer, rows, adapters
+
+
+def adapter_plan(rows, adapters, buffer=None):
+    """xbar_adapter_plan: rows[M] int32, the adapter of every row (none: a number outside [0, adapters))."""
+    assert rows.dim() == 1
+    _here(rows, buffer)
+    M = rows.shape[0]
+    address = _dev(rows, torch.int32)
+
+    def size():
+        nbytes = lib().xbar_adapter_plan_bytes(M, adapters)
+        _check(0 if nbytes else -2)
+        return nbytes
+    buffer = _buffer(size, buffer, rows.device)
+    _check(lib().xbar_adapter_plan(address, M, adapters, buffer.data_ptr(), buffer.numel(), _stream()))
+    return AdapterPlan(buffer, M, adapters)
+
+
+def _adapter(plan, op, X_cols, Y_cols, A, B, scale, ws):
+    """(type, rank, workspace) of a call, its shapes checked."""
+    n, rank, K = A.shape
+    assert n == plan.adapters and B.shape[:2] == (n, rank) and scale.shape == (n,), "adapters of another number or rank than the plan's"
+    assert K == X_cols and B.shape[2] == Y_cols and A.dtype is B.dtype and A.dtype in (torch.float32, torch.bfloat16)
+
+    def size():
+        nbytes = lib().xbar_adapter_workspace_bytes(op, plan.rows, K, Y_cols, rank, n)
+        _check(0 if nbytes else -2)
+        return nbytes
+    return BF16 if A.dtype is torch.bfloat16 else F32, rank, _buffer(size, ws, A.device)
+
+
+def adapter_fwd(plan, base, X, A, B, scale, out=None, ws=None):
+    """xbar_adapter_fwd: (Y, T), Y[M][N] = base + every row's adapter on X[M][K]; out: base itself (in place) or another tensor."""
+    M, N = base.shape
+    assert X.dim() == 2 and X.shape[0] == M == plan.rows
+    kind, rank, ws = _adapter(plan, OP_FWD, X.shape[1], N, A, B, scale, ws)
+    _here(plan.buffer, base, X, A, B, scale, out, ws)
+    out = torch.empty_like(base) if out is None else out
+    assert out.shape == base.shape
+    T = torch.empty((M, rank), dtype=torch.float32, device=X.device)
+    _check(lib().xbar_adapter_fwd(plan.buffer.data_ptr(), plan.buffer.numel(), _dev(base), _dev(X), _dev(A, A.dtype), _dev(B, A.dtype), kind,
+                                  _dev(scale), _dev(out), _dev(T), M, X.shape[1], N, rank, plan.adapters, ws.data_ptr(), ws.numel(), _stream()))
+    return out, T
+
+
+def adapter_bwd(plan, base, dY, X, T, A, B, scale, out=None, ws=None):
+    """xbar_adapter_bwd: (dX, dA, dB), dX[M][K] = base + the errors through every row's adapter; base None: dX is not wanted (None)."""
+    M, K = X.shape
+    N = dY.shape[1]
+    assert dY.shape[0] == M == plan.rows and T.shape == (M, A.shape[1]) and (base is None or base.shape == X.shape)
+    kind, rank, ws = _adapter(plan, OP_BWD, K, N, A, B, scale, ws)
+    _here(plan.buffer, base, dY, X, T, A, B, scale, out, ws)
+    assert base is not None or out is None
+    if base is not None and out is None:
+        out = torch.empty_like(base)
+    assert out is None or out.shape == X.shape
+    dA = torch.empty(A.shape, dtype=torch.float32, device=X.device)
+    dB = torch.empty(B.shape, dtype=torch.float32, device=X.device)
+    _check(lib().xbar_adapter_bwd(plan.buffer.data_ptr(), plan.buffer.numel(), None if base is None else _dev(base), _dev(dY), _dev(X), _dev(T),
+                                  _dev(A, A.dtype), _dev(B, A.dtype), kind, _dev(scale), None if out is None else _dev(out), _dev(dA), _dev(dB),
+                                  M, K, N, rank, plan.adapters, ws.data_ptr(), ws.numel(), _stream()))
+    return out, dA, dB
+
+
+class TensorList:
+    """Addresses and sizes of a list of tensors as the library takes them, for programs that step the same tensors again and again: the tensors
+    must keep their memory as long as the list is used."""
+
+    def __init__(self, tensors):
+        self.tensors = tuple(tensors)
+        assert self.tensors, "a list of tensors"
+        _here(*self.tensors)
+        self.addresses = (C.c_void_p * len(self.tensors))(*[_dev(t) for t in self.tensors])
+        self.sizes = (C.c_size_t * len(self.tensors))(*[t.numel() for t in self.tensors])
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+def _grads_call(grads, ws):
+    grads = grads if isinstance(grads, TensorList) else TensorList(grads)
+    device = grads.tensors[0].device
+    _here(grads.tensors[0], ws)
+
+    def size():
+        nbytes = lib().xbar_grads_workspace_bytes(len(grads))
+        _check(0 if nbytes else -2)
+        return nbytes
+    return grads, torch.empty(1, dtype=torch.float32, device=device), _buffer(size, ws, device)
+
+
+def grad_norm(grads, ws=None):
+    """xbar_grad_norm: the global norm of a list of tensors (or a TensorList), a tensor of one element."""
+    grads, norm, ws = _grads_call(grads, ws)
+    _check(lib().xbar_grad_norm(grads.addresses, grads.sizes, len(grads), _dev(norm), ws.data_ptr(), ws.numel(), _stream()))
+    return norm
+
+
+def grad_clip(grads, max_norm, ws=None):
+    """xbar_grad_clip: the gradients in place to a global norm of at most max_norm; returns the norm they had."""
+    grads, norm, ws = _grads_call(grads, ws)
+    _check(lib().xbar_grad_clip(grads.addresses, grads.sizes, len(grads), max_norm, _dev(norm), ws.data_ptr(), ws.numel(), _stream()))
+    return norm
+
+
+def clip_sgd(params, grads, lr, max_norm=float("inf"), ws=None):
+    """xbar_clip_sgd: the SGD step of a list of parameters with their gradients clipped to a global norm of at most max_norm; returns
+    the norm the gradients had."""
+    grads, norm, ws = _grads_call(grads, ws)
+    params = params if isinstance(params, TensorList) else TensorList(params)
+    assert len(params) == len(grads) and bytes(params.sizes) == bytes(grads.sizes), "parameters and gradients of different sizes"
+    _check(lib().xbar_clip_sgd(params.addresses, grads.addresses, grads.sizes, len(grads), lr, max_norm, _dev(norm), ws.data_ptr(), ws.numel(),
+                               _stream()))
+    return norm
 
 
 ADC_HIST_BINS = 4096

@@ -1,0 +1,164 @@
+"""Digital operators beside the crossbar layers, without a GPU: their definitions against differences, the library's refusals, the
+binding's checks, the plan of the launches."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+from oracle import digital
+
+
+@pytest.fixture(scope="module")
+def xb():
+    import os
+    from paper_2002_11151_amd import xbar
+    if not os.path.exists(xbar.LIB_PATH):
+        import __graft_entry__
+        __graft_entry__.build()
+    xbar.lib()
+    return xbar
+
+
+def differences(f, at, h=1e-5):
+    """Gradient of the scalar f at the array `at` by central differences."""
+    out = np.zeros_like(at)
+    flat, grad = at.reshape(-1), out.reshape(-1)
+    for i in range(flat.size):
+        keep = flat[i]
+        flat[i] = keep + h
+        up = f()
+        flat[i] = keep - h
+        grad[i] = (up - f()) / (2 * h)
+        flat[i] = keep
+    return out
+
+
+@pytest.mark.parametrize("kind", ["none", "relu", "silu"])
+def test_group_norm_gradient_is_that_of_the_formula(kind):
+    rng = np.random.default_rng(3)
+    x, skip, dy = (rng.normal(size=(2, 2, 3, 6)) for _ in range(3))
+    gamma, beta = rng.uniform(0.5, 1.5, 6), rng.normal(size=6)
+
+    def loss():
+        mean, invstd = digital.gn_stats(x, 3, 1e-5)
+        return float((digital.act(digital.gn_z(x, gamma, beta, mean, invstd, skip)[1], kind) * dy).sum())
+    mean, invstd = digital.gn_stats(x, 3, 1e-5)
+    got = digital.gn_bwd(x, dy, gamma, beta, mean, invstd, kind, skip)
+    for g, at in zip(got, (x, gamma, beta, skip)):
+        # truncation h^2 f''' / 6 and rounding 1e-16 |loss| / h
+        assert np.abs(g - differences(loss, at)).max() < 1e-6
+
+
+def test_adapter_gradients_are_those_of_the_formula():
+    rng = np.random.default_rng(4)
+    rows = np.array([1, -1, 0, 1, 5, 1])
+    X, dY = rng.normal(size=(6, 4)), rng.normal(size=(6, 5))
+    A, B, scale = rng.normal(size=(2, 3, 4)), rng.normal(size=(2, 3, 5)), rng.uniform(0.5, 2, 2)
+    base, back = rng.normal(size=(6, 5)), np.zeros((6, 4))
+    loss = lambda: float((digital.adapter_fwd(rows, base, X, A, B, scale)[0] * dY).sum())
+    T = digital.adapter_fwd(rows, base, X, A, B, scale)[1]
+    dX, dA, dB, _ = digital.adapter_bwd(rows, back, dY, X, T, A, B, scale)
+    for g, at in ((dX, X), (dA, A), (dB, B)):
+        assert np.abs(g - differences(loss, at)).max() < 1e-6
+    assert not dX[1].any() and not dX[4].any()                   # rows without an adapter
+
+
+P = 0x10000                                                      # an address that is never looked at: every call below is refused
+
+
+def test_group_norm_refusals(xb):
+    lib = xb.lib()
+    big = 1 << 40
+    ok = dict(x=P, gamma=P, beta=P, skip=None, y=2 * big, mean=P, invstd=P, batch=2, positions=9, channels=12, groups=3, eps=1e-5, act=0, ws=P, n=big)
+
+    def fwd(**kw):
+        a = dict(ok, **kw)
+        return lib.xbar_gn_fwd(a["x"], a["gamma"], a["beta"], a["skip"], a["y"], a["mean"], a["invstd"], a["batch"], a["positions"], a["channels"],
+                               a["groups"], a["eps"], a["act"], a["ws"], a["n"], None)
+    assert fwd(batch=0) == fwd(positions=0) == fwd(channels=0) == fwd(groups=0) == fwd(groups=5) == fwd(groups=24) == -2
+    assert fwd(batch=1 << 24, groups=1) == fwd(batch=1 << 20, positions=1 << 16) == fwd(channels=(1 << 20) + 3) == -2
+    assert fwd(x=None) == fwd(gamma=P + 4) == fwd(skip=P + 8) == fwd(y=None) == fwd(mean=None) == fwd(ws=P + 1) == -3
+    assert fwd(eps=-1.0) == fwd(eps=float("nan")) == fwd(act=3) == fwd(act=-1) == -1
+    assert fwd(y=P) == fwd(y=P + 16) == fwd(skip=2 * big + 16) == -1
+    assert fwd(n=lib.xbar_gn_workspace_bytes(2, 9, 12, 3) - 1) == -4
+    assert lib.xbar_gn_workspace_bytes(2, 9, 12, 5) == 0 and lib.xbar_gn_workspace_bytes(2, 9, 12, 3) > 0
+
+    bok = dict(x=P, dy=P, gamma=P, beta=P, skip=None, mean=P, invstd=P, dx=2 * big, dgamma=P, dbeta=P, dskip=None, groups=3, act=0, ws=P, n=big)
+
+    def bwd(**kw):
+        a = dict(bok, **kw)
+        return lib.xbar_gn_bwd(a["x"], a["dy"], a["gamma"], a["beta"], a["skip"], a["mean"], a["invstd"], a["dx"], a["dgamma"], a["dbeta"], a["dskip"],
+                               2, 9, 12, a["groups"], a["act"], a["ws"], a["n"], None)
+    assert bwd(groups=7) == -2
+    assert bwd(dy=None) == bwd(dx=P + 4) == bwd(dgamma=None) == bwd(dbeta=P + 8) == bwd(dskip=P + 4, skip=P) == bwd(invstd=None) == -3
+    assert bwd(dskip=P) == bwd(act=7) == bwd(dx=P) == bwd(skip=P, dskip=P) == bwd(skip=P, dskip=2 * big) == -1
+    assert bwd(n=0) == -4
+
+
+def test_adapter_refusals(xb):
+    lib = xb.lib()
+    size = lambda M=8, K=16, N=24, rank=4, n=3, op=xb.OP_FWD: lib.xbar_adapter_workspace_bytes(op, M, K, N, rank, n)
+    assert size(M=0) == size(K=0) == size(N=0) == size(rank=0) == size(rank=129) == size(n=0) == size(n=65537) == size(K=1 << 24) == 0
+    assert size(op=xb.OP_UPDATE) == 0 and size() > 0 and size(op=xb.OP_BWD) > size()
+    assert lib.xbar_adapter_plan_bytes(0, 1) == lib.xbar_adapter_plan_bytes((1 << 24) + 1, 1) == lib.xbar_adapter_plan_bytes(1, 0) == 0
+    plan = lib.xbar_adapter_plan_bytes(8, 3)
+    assert lib.xbar_adapter_plan(P, 0, 3, P, plan, None) == -2
+    assert lib.xbar_adapter_plan(None, 8, 3, P, plan, None) == lib.xbar_adapter_plan(P, 8, 3, P + 4, plan, None) == -3
+    assert lib.xbar_adapter_plan(P, 8, 3, P, plan - 1, None) == -4
+    far = [(i + 1) << 32 for i in range(12)]
+    ok = dict(plan=far[0], plan_bytes=plan, base=far[1], X=far[2], A=far[3], B=far[4], type=0, scale=far[5], Y=far[6], T=far[7], M=8, K=16, N=24, rank=4,
+              n=3, ws=far[8], ws_bytes=size())
+
+    def fwd(**kw):
+        a = dict(ok, **kw)
+        return lib.xbar_adapter_fwd(a["plan"], a["plan_bytes"], a["base"], a["X"], a["A"], a["B"], a["type"], a["scale"], a["Y"], a["T"], a["M"], a["K"],
+                                    a["N"], a["rank"], a["n"], a["ws"], a["ws_bytes"], None)
+    assert fwd(M=0) == fwd(rank=129) == fwd(n=0) == -2
+    assert fwd(type=2) == fwd(Y=far[2]) == fwd(Y=far[1] + 16) == fwd(T=far[6]) == fwd(T=far[2]) == fwd(Y=far[3]) == -1
+    assert fwd(plan=None) == fwd(base=None) == fwd(X=far[2] + 4) == fwd(A=None) == fwd(scale=None) == fwd(Y=None) == fwd(T=far[7] + 4) == fwd(ws=None) == -3
+    assert fwd(plan_bytes=plan - 1) == fwd(ws_bytes=size() - 1) == -4
+    bok = dict(ok, dY=far[6], T=far[7], dX=far[9], dA=far[10], dB=far[11], base=far[1], ws_bytes=size(op=xb.OP_BWD))
+
+    def bwd(**kw):
+        a = dict(bok, **kw)
+        return lib.xbar_adapter_bwd(a["plan"], a["plan_bytes"], a["base"], a["dY"], a["X"], a["T"], a["A"], a["B"], a["type"], a["scale"], a["dX"], a["dA"],
+                                    a["dB"], a["M"], a["K"], a["N"], a["rank"], a["n"], a["ws"], a["ws_bytes"], None)
+    assert bwd(K=0) == -2
+    assert bwd(type=-1) == bwd(dX=far[2]) == bwd(dA=far[3]) == bwd(dB=far[10]) == bwd(dX=far[1] + 64) == -1
+    assert bwd(base=None) == bwd(T=None) == bwd(dA=None) == bwd(dB=None) == bwd(dX=far[9] + 4) == -3
+    assert bwd(ws_bytes=size(op=xb.OP_BWD) - 1) == -4
+
+
+def test_gradient_list_refusals(xb):
+    lib = xb.lib()
+
+    def lists(*tensors):
+        return (C.c_void_p * len(tensors))(*[t[0] for t in tensors]), (C.c_size_t * len(tensors))(*[t[1] for t in tensors])
+    far, n = 1 << 40, lib.xbar_grads_workspace_bytes(2)
+    g, sizes = lists((P, 4), (2 * P, 5))
+    p, _ = lists((3 * P, 4), (4 * P, 5))
+    norm = lambda g=g, sizes=sizes, k=2, out=far, ws=2 * far, n=n: lib.xbar_grad_norm(g, sizes, k, out, ws, n, None)
+    clip = lambda g=g, sizes=sizes, k=2, most=1.0, out=far, ws=2 * far, n=n: lib.xbar_grad_clip(g, sizes, k, most, out, ws, n, None)
+    step = lambda p=p, g=g, sizes=sizes, k=2, lr=0.1, most=1.0, out=far, ws=2 * far, n=n: lib.xbar_clip_sgd(p, g, sizes, k, lr, most, out, ws, n, None)
+    assert norm(k=0) == norm(k=2049) == lib.xbar_grads_workspace_bytes(0) - 2 == lib.xbar_grads_workspace_bytes(2049) - 2 == -2
+    assert norm(sizes=lists((0, 4), (0, 1 << 38))[1]) == -2
+    assert norm(g=None) == norm(sizes=None) == step(p=None) == -1
+    assert norm(out=None) == norm(ws=None) == norm(ws=2 * far + 4) == norm(g=lists((P, 0), (None, 0))[0]) == norm(g=lists((P + 4, 0), (P, 0))[0]) == -3
+    assert step(p=lists((3 * P, 0), (4 * P + 8, 0))[0]) == -3
+    assert norm(n=n - 1) == clip(n=0) == step(n=n - 1) == -4
+    assert clip(most=0.0) == clip(most=float("nan")) == clip(most=-1.0) == step(most=0.0) == step(lr=float("inf")) == step(lr=float("nan")) == -1
+    # the same memory twice: among the gradients that are scaled, the parameters, parameters and gradients, results and workspace
+    assert clip(g=lists((P, 0), (P, 0))[0]) == clip(g=lists((P, 0), (P - 16, 0))[0]) == clip(out=P) == clip(ws=P) == -1
+    assert step(p=lists((3 * P, 0), (3 * P, 0))[0]) == step(p=lists((3 * P, 0), (2 * P + 16, 0))[0]) == step(out=3 * P) == step(ws=P) == -1
+
+
+def test_binding_checks_lists_and_devices(xb):
+    torch = pytest.importorskip("torch")
+    with pytest.raises((AssertionError, RuntimeError)):
+        xb.TensorList([])
+    with pytest.raises((AssertionError, RuntimeError)):          # host tensors
+        xb.grad_norm([torch.zeros(4)])
+    with pytest.raises((AssertionError, RuntimeError)):
+        xb.gn_fwd(torch.zeros(2, 4), torch.ones(4), torch.zeros(4), 2)
+    with pytest.raises((AssertionError, RuntimeError)):
+        xb.adapter_plan(torch.zeros(4, dtype=torch.int32), 2)

@@ -1,0 +1,351 @@
+"""GPU parity of the digital operators beside the crossbar layers (group norm with an activation, low-rank adapters, global gradient norm and
+clipped step) against their float64 definitions, at the sizes, orders and values where they can go wrong."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import digital
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24                       # half a step of a float, relative
+
+
+@pytest.fixture(scope="module")
+def xb():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2002_11151_amd import xbar
+    xbar.lib()
+    return xbar
+
+
+def dev(a, dtype=np.float32):
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=dtype)).cuda()
+
+
+def host(t):
+    return t.float().cpu().numpy().astype(np.float64)
+
+
+def within(got, want, bound, what=""):
+    got = host(got)
+    assert got.shape == want.shape, what
+    off = np.abs(got - want) - bound
+    assert np.isfinite(got).all() and (off <= 0).all(), "%s: %g over the bound, at %s" % (what, off.max(), np.unravel_index(off.argmax(), off.shape))
+
+
+# ---- group norm ------------------------------------------------------------------------------------
+KINDS = ("none", "relu", "silu")
+
+
+def gn_case(shape, seed, skip):
+    rng = np.random.default_rng(seed)
+    x = (rng.normal(size=shape) * 2 + rng.normal(size=shape[-1])).astype(np.float32)
+    dy = rng.normal(size=shape).astype(np.float32)
+    gamma, beta = rng.uniform(0.5, 1.5, size=shape[-1]).astype(np.float32), rng.normal(size=shape[-1]).astype(np.float32)
+    gamma[::3] *= -1
+    return x, dy, gamma, beta, rng.normal(size=shape).astype(np.float32) if skip else None
+
+
+def gn_check(xb, shape, groups, kind, skip, seed=0):
+    x, dy, gamma, beta, s = gn_case(shape, seed, skip)
+    act = KINDS.index(kind)
+    sd = None if s is None else dev(s)
+    y, mean, invstd = xb.gn_fwd(dev(x), dev(gamma), dev(beta), groups, 1e-5, act, sd)
+    m64, i64 = digital.gn_stats(x, groups, 1e-5)
+    within(mean, m64, 2 * U * np.abs(m64) + 1e-12, "mean")
+    within(invstd, i64, 2.1 * U * i64, "invstd")
+    m, i = host(mean), host(invstd)                                     # rounded statistics are what is used, in both directions
+    xhat, z = digital.gn_z(x, gamma, beta, m, i, s)
+    want = digital.act(z, kind)
+    # one rounding of z; the smooth activation adds its exponential (2 U, and U |z| from its argument), a sum and a division
+    slack = 1.01 * U * np.abs(want) + 1e-13 if kind != "silu" else U * (8 * np.abs(want) + 1.2 * np.abs(z)) + 1e-36
+    within(y, want, slack, "y")
+    got = xb.gn_bwd(dev(x), dev(dy), dev(gamma), dev(beta), mean, invstd, act, sd)
+    dx, dgamma, dbeta, dskip = digital.gn_bwd(x, dy, gamma, beta, m, i, kind, s)
+    e = np.abs(dy) * U * (16 + 8 * np.abs(z)) if kind == "silu" else np.zeros_like(z)      # error of the error behind the activation
+    if skip:
+        within(got[3], dskip, e + 1.01 * U * np.abs(dskip), "dskip")
+    n, c = shape[0], shape[-1]
+    mean_of = lambda t: digital._spread(t.reshape(n, -1, groups, c // groups).mean((1, 3)), x, groups)
+    ge = np.abs(gamma) * e
+    far = digital._spread(i, x, groups) * (ge + mean_of(ge) + np.abs(xhat) * mean_of(ge * np.abs(xhat)))
+    size = digital._spread(i, x, groups) * np.abs(gamma) * np.abs(dy).max()                # of the terms, in double precision
+    within(got[0], dx, far + 1.01 * U * np.abs(dx) + 1e-12 * size * (1 + np.abs(xhat)), "dx")
+    axes = tuple(range(x.ndim - 1))
+    within(got[1], dgamma, (e * np.abs(xhat)).sum(axes) + 1.01 * U * np.abs(dgamma) + 1e-12 * (np.abs(dy * xhat)).sum(axes), "dgamma")
+    within(got[2], dbeta, e.sum(axes) + 1.01 * U * np.abs(dbeta) + 1e-12 * np.abs(dy).sum(axes), "dbeta")
+
+
+# one value a group; channels that are no quads; groups across and inside a quad; one position; positions that end inside a block's share; many
+# channels; many samples of next to nothing; the networks' own layers
+@pytest.mark.parametrize("shape,groups", [
+    ((1, 1), 1), ((3, 7), 7), ((1, 64), 4), ((2, 5, 3, 6), 3), ((2, 4, 4, 64), 32), ((3, 7, 5, 30), 5), ((2, 9, 9, 12), 1), ((1, 8, 8, 64), 16),
+    ((5, 33, 31, 20), 5), ((2, 56, 56, 64), 32), ((1, 7, 7, 2048), 32), ((700, 3, 40), 8), ((1, 257, 129, 3), 3), ((4, 13, 11, 1030), 103),
+    ((2, 28, 28, 512), 32), ((1, 64, 64, 128), 2), ((3, 20, 20, 96), 4), ((16, 1, 1, 4096), 64), ((2, 600, 68), 17)])
+@pytest.mark.parametrize("kind,skip", [("none", False), ("relu", True), ("silu", False)])
+def test_group_norm(xb, shape, groups, kind, skip):
+    gn_check(xb, shape, groups, kind, skip)
+
+
+@pytest.mark.parametrize("kind,skip", [("none", True), ("relu", False), ("silu", True)])
+def test_group_norm_other_branches(xb, kind, skip):
+    gn_check(xb, (3, 11, 9, 48), 6, kind, skip, 1)
+    gn_check(xb, (2, 70, 61, 50), 10, kind, skip, 2)
+
+
+def test_group_norm_of_a_constant_and_of_a_large_mean(xb):
+    """A group without spread has xhat = 0 and 1 / sqrt(eps); one whose mean is 2^20 times its spread keeps the digits of the spread."""
+    x = np.full((2, 6, 6, 8), 3.25, dtype=np.float32)
+    one, zero = np.ones(8, np.float32), np.zeros(8, np.float32)
+    y, mean, invstd = xb.gn_fwd(dev(x), dev(one), dev(zero), 2, 1e-5)
+    assert not host(y).any() and (host(mean) == 3.25).all() and np.abs(host(invstd) * np.sqrt(1e-5) - 1).max() < 2.1 * U
+    rng = np.random.default_rng(7)
+    for shape in ((1, 40, 40, 32), (2, 130, 130, 64)):
+        x = (1024.0 + rng.integers(0, 16, size=shape) * 2.0 ** -13).astype(np.float32)      # exact in float
+        _, mean, invstd = xb.gn_fwd(dev(x), dev(np.ones(shape[-1])), dev(np.zeros(shape[-1])), 4, 0.0)
+        m64, i64 = digital.gn_stats(x, 4, 0.0)
+        within(mean, m64, 2 * U * np.abs(m64))
+        within(invstd, i64, 2.1 * U * i64)
+
+
+def test_group_norm_keeps_nan_to_its_group(xb):
+    x, dy, gamma, beta, _ = gn_case((2, 6, 5, 16), 3, False)
+    x[1, 2, 3, 5] = np.nan
+    y, mean, invstd = xb.gn_fwd(dev(x), dev(gamma), dev(beta), 4)
+    bad = np.zeros((2, 4), bool)
+    bad[1, 1] = True
+    assert np.array_equal(np.isnan(mean.cpu().numpy()), bad) and np.array_equal(np.isnan(invstd.cpu().numpy()), bad)
+    lost = np.zeros(x.shape, bool)
+    lost[1, :, :, 4:8] = True
+    assert np.array_equal(np.isnan(y.cpu().numpy()), lost)
+    dx, dgamma, _ = xb.gn_bwd(dev(x), dev(dy), dev(gamma), dev(beta), mean, invstd)
+    assert np.array_equal(np.isnan(dx.cpu().numpy()), lost) and np.isnan(dgamma.cpu().numpy()).sum() == 4
+    r = xb.gn_fwd(dev(x), dev(gamma), dev(beta), 4, 1e-5, xb.ACT_RELU)[0]
+    assert not r.cpu().numpy()[lost].any()                                                  # as relu_fwd
+
+
+# ---- adapters --------------------------------------------------------------------------------------
+def adapter_case(rows, K, N, rank, n, seed, bf16=False):
+    rng = np.random.default_rng(seed)
+    M = len(rows)
+    f = lambda *s: rng.normal(size=s).astype(np.float32)
+    A, B = dev(f(n, rank, K) / np.sqrt(K)), dev(f(n, rank, N) / np.sqrt(rank))
+    if bf16:
+        A, B = A.bfloat16(), B.bfloat16()
+    return dict(rows=np.asarray(rows, dtype=np.int32), X=f(M, K), base=f(M, N), back=f(M, K), dY=f(M, N), A=A, B=B,
+                scale=rng.uniform(0.5, 2, n).astype(np.float32))
+
+
+def adapter_check(xb, c, in_place=False):
+    A, B, rows = c["A"], c["B"], c["rows"]
+    n, rank, K = A.shape
+    N, M = B.shape[2], len(rows)
+    A64, B64 = host(A), host(B)
+    plan = xb.adapter_plan(dev(rows, np.int32), n)
+    base, X, scale, dY, back = (dev(c[k]) for k in ("base", "X", "scale", "dY", "back"))
+    Y, T = xb.adapter_fwd(plan, base, X, A, B, scale, out=base if in_place else None)
+    want, T64 = digital.adapter_fwd(rows, c["base"], c["X"], A64, B64, c["scale"])
+    # sums of n products in single precision, whatever their order: n U times the sum of their sizes; a quarter of the terms at most is added one
+    # after another (four of them meet in an instruction), then shares and waves
+    aX, aA, aB, s64 = np.abs(c["X"]).astype(np.float64), np.abs(A64), np.abs(B64), np.abs(c["scale"]).astype(np.float64)
+    chain = lambda k: (k / 4 + 48) * U
+    sizes, aT = digital.adapter_fwd(rows, np.zeros_like(want), aX, aA, aB, s64)
+    within(T, T64, chain(K) * aT + 1e-30, "T")
+    within(Y, want, (chain(K) + chain(rank) + 4 * U) * sizes + 2 * U * (np.abs(c["base"]) + np.abs(want)), "Y")
+    out = (rows < 0) | (rows >= n)
+    assert np.array_equal(host(Y)[out], c["base"][out].astype(np.float64)) and not host(T)[out].any()
+    T32 = host(T)
+    dX, dA, dB = xb.adapter_bwd(plan, back, dY, X, T, A, B, scale, out=back if in_place else None)
+    dXw, dAw, dBw, dT = digital.adapter_bwd(rows, c["back"], c["dY"], c["X"], T32, A64, B64, c["scale"])
+    aY = np.abs(c["dY"]).astype(np.float64)
+    sx, sa, sb, _ = digital.adapter_bwd(rows, np.zeros_like(dXw), aY, aX, np.abs(T32), aA, aB, s64)
+    within(dX, dXw, (chain(N) + chain(rank) + 4 * U) * sx + 2 * U * (np.abs(c["back"]) + np.abs(dXw)), "dX")
+    within(dA, dAw, (chain(N) + chain(M) + 4 * U) * sa + 1e-30, "dA")
+    within(dB, dBw, (chain(M) + 4 * U) * sb + 1e-30, "dB")
+    assert np.array_equal(host(dX)[out], c["back"][out].astype(np.float64))
+    none, dA2, dB2 = xb.adapter_bwd(plan, None, dY, X, T, A, B, scale)
+    assert none is None and torch.equal(dA, dA2) and torch.equal(dB, dB2)                   # without dX, and in a fixed order
+
+
+def mixed(M, n, seed, share=0.15):
+    rng = np.random.default_rng(seed)
+    rows = rng.integers(0, n, size=M)
+    rows[rng.random(M) < share] = -1
+    return rows
+
+
+@pytest.mark.parametrize("M,K,N,rank,n", [
+    (1, 1, 1, 1, 1), (1, 2048, 1000, 8, 4), (3, 17, 5, 3, 2), (16, 64, 64, 16, 1), (17, 100, 36, 17, 3), (33, 63, 65, 5, 40), (64, 784, 500, 8, 3),
+    (70, 36, 300, 33, 5), (130, 500, 10, 64, 2), (40, 129, 257, 100, 2), (50, 260, 130, 128, 7), (300, 48, 52, 4, 1), (700, 31, 70, 7, 3),
+    (1500, 20, 24, 12, 900)])
+@pytest.mark.parametrize("bf16", [False, True])
+def test_adapters(xb, M, K, N, rank, n, bf16):
+    adapter_check(xb, adapter_case(mixed(M, n, M + n), K, N, rank, n, M, bf16))
+
+
+def test_adapters_without_rows_and_rows_without_adapters(xb):
+    adapter_check(xb, adapter_case([-1] * 40, 20, 28, 4, 2, 1))                              # no row has one
+    adapter_check(xb, adapter_case([5, -7, 2 ** 31 - 1, 0, -2 ** 31, 0], 20, 28, 4, 2, 2))    # numbers outside the range
+    adapter_check(xb, adapter_case([2] * 33, 20, 28, 4, 6, 3), in_place=True)                # all rows one adapter, the others none
+    adapter_check(xb, adapter_case(np.arange(130) % 65 - 1, 40, 44, 9, 64, 4), in_place=True)
+
+
+@pytest.mark.parametrize("M", [31, 32, 33, 64, 65, 255, 256, 257, 512, 513, 1023, 1024, 1025])
+def test_adapter_tiles_and_chunks_end_everywhere(xb, M):
+    adapter_check(xb, adapter_case(np.minimum(np.arange(M) // 256, 1), 24, 20, 4, 2, M))
+
+
+def test_adapters_with_many_rows_in_any_order(xb):
+    rng = np.random.default_rng(9)
+    rows = rng.permutation(np.repeat([0, 1, 2, -1], [8000, 37, 1, 1200]))
+    adapter_check(xb, adapter_case(rows, 12, 8, 3, 4, 5))
+
+
+def test_adapters_keep_infinities_to_their_rows(xb):
+    """A row, an adapter or a rank that holds an infinity or a NaN spoils nothing else; what lies behind the last rank or column is not read."""
+    c = adapter_case([0, 1, 0, -1, 2, 1], 22, 26, 5, 3, 6)
+    clean = {k: (v.clone() if torch.is_tensor(v) else v.copy()) for k, v in c.items()}
+    c["X"][1, 4], c["X"][3, 0], c["dY"][1, 2], c["dY"][3, 1] = np.inf, np.nan, np.nan, np.inf
+    c["A"][2, 3, 7] = float("nan")
+    c["B"][2, 4, 9] = float("inf")
+
+    def run(c):
+        plan = xb.adapter_plan(dev(c["rows"], np.int32), 3)
+        X, scale = dev(c["X"]), dev(c["scale"])
+        Y, T = xb.adapter_fwd(plan, dev(c["base"]), X, c["A"], c["B"], scale)
+        return (Y, T) + xb.adapter_bwd(plan, dev(c["back"]), dev(c["dY"]), X, T, c["A"], c["B"], scale)
+    got, want = run(c), run(clean)
+    for g, w in zip(got[:3], want[:3]):
+        assert torch.equal(g[[0, 2, 3, 5]], w[[0, 2, 3, 5]])
+        assert torch.isfinite(w).all()
+    for g, w in zip(got[3:], want[3:]):
+        assert torch.equal(g[0], w[0])
+
+
+def test_plan_of_another_batch_writes_nothing(xb):
+    c = adapter_case([0, 1, 0, 1], 20, 24, 4, 2, 8)
+    plan = xb.adapter_plan(dev(c["rows"], np.int32), 2)
+    other = xb.adapter_plan(dev([0, 1, 0, 1, 1], np.int32), 2)
+    other.rows = 4                                                                           # (the binding itself refuses it)
+    with pytest.raises(AssertionError):
+        xb.adapter_fwd(xb.adapter_plan(dev([0, 1, 0], np.int32), 2), dev(c["base"]), dev(c["X"]), c["A"], c["B"], dev(c["scale"]))
+    out = torch.full((4, 24), 7.0, device="cuda")
+    xb.adapter_fwd(other, dev(c["base"]), dev(c["X"]), c["A"], c["B"], dev(c["scale"]), out=out)
+    assert (out == 7.0).all()
+    xb.adapter_fwd(plan, dev(c["base"]), dev(c["X"]), c["A"], c["B"], dev(c["scale"]), out=out)
+    assert (out != 7.0).any()
+
+
+# ---- gradients of many tensors ---------------------------------------------------------------------
+def grads_of(sizes, seed):
+    rng = np.random.default_rng(seed)
+    return [(rng.normal(size=n) * 10.0 ** rng.integers(-3, 2)).astype(np.float32) for n in sizes]
+
+
+SIZES = [[1], [4], [3, 0, 5], [16384], [16385, 1, 16383], [64] * 40, [100003, 7, 65536, 2], list(range(1, 260)), [5] * 130 + [0] * 20 + [70000]]
+
+
+@pytest.mark.parametrize("sizes", SIZES, ids=lambda s: "%dx%d" % (len(s), max(s)))
+def test_gradient_norm_and_clipping(xb, sizes):
+    grads = grads_of(sizes, len(sizes))
+    params = grads_of(sizes, 1000 + len(sizes))
+    want = digital.grad_norm(grads)
+    g = [dev(t) for t in grads]
+    got = float(xb.grad_norm(g).cpu()[0])
+    assert abs(got - want) <= 1.01 * U * want
+    for most in (want / 3, want * 3):
+        c = digital.clip_factor(want, most)
+        p = [dev(t) for t in params]
+        norm = xb.clip_sgd(p, g, 0.125, most)
+        assert float(norm.cpu()[0]) == got
+        for a, b, q in zip(p, grads, params):                         # max_norm is a float; lr c rounded, its product with g, the sum
+            step = 0.125 * c * b.astype(np.float64)
+            within(a, q - step, U * (np.abs(q - step) + 4 * np.abs(step)), "p")
+        assert all(np.array_equal(a.cpu().numpy(), b) for a, b in zip(g, grads))              # the step leaves the gradients alone
+        h = [t.clone() for t in g]
+        assert float(xb.grad_clip(h, most).cpu()[0]) == got
+        assert all(torch.equal(xb.sgd(dev(q), b, 0.125), a) for q, b, a in zip(params, h, p) if b.numel())
+        for a, b in zip(h, grads):
+            if c == 1.0:
+                assert np.array_equal(a.cpu().numpy(), b)
+            else:
+                within(a, c * b.astype(np.float64), 4 * U * np.abs(c * b.astype(np.float64)) + 1e-45, "g")
+
+
+def test_step_without_a_limit_is_the_plain_one(xb):
+    g, p = [dev(t) for t in grads_of([1000, 33], 5)], [dev(t) for t in grads_of([1000, 33], 6)]
+    want = [xb.sgd(t.clone(), u, 0.03) for t, u in zip(p, g)]
+    xb.clip_sgd(p, g, 0.03)
+    assert all(torch.equal(a, b) for a, b in zip(p, want))
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+def test_gradients_that_are_no_numbers_move_nothing(xb, bad):
+    grads, params = grads_of([700, 20000], 7), grads_of([700, 20000], 8)
+    grads[1][12345] = bad
+    g, p = [dev(t) for t in grads], [dev(t) for t in params]
+    for norm in (xb.grad_norm(g), xb.grad_clip(g, 1.0), xb.clip_sgd(p, g, 0.1, 1.0)):
+        assert not np.isfinite(float(norm.cpu()[0]))
+    assert all(np.array_equal(a.cpu().numpy(), b, equal_nan=True) for a, b in zip(g + p, grads + params))
+
+
+def test_gradients_beyond_the_range_of_their_squares(xb):
+    for size in (1e30, 1e-30):
+        g = [torch.full((5000,), size, device="cuda"), torch.full((3,), size, device="cuda")]
+        want = float(np.float32(size)) * np.sqrt(5003)
+        assert abs(float(xb.grad_clip(g, 1e-33).cpu()[0]) - want) <= 1.01 * U * want
+        assert np.abs(host(g[0]) * np.sqrt(5003) / float(np.float32(1e-33)) - 1).max() < 1e-5    # (results near the smallest normal numbers)
+
+
+def test_empty_lists_of_elements(xb):
+    e = torch.empty(0, device="cuda")
+    assert float(xb.grad_norm([e]).cpu()[0]) == 0.0 and float(xb.clip_sgd([e, e], [e, e], 0.1, 1.0).cpu()[0]) == 0.0
+
+
+# ---- how programs call them ------------------------------------------------------------------------
+def test_another_stream_and_a_captured_graph(xb):
+    """Every operator on a side stream, captured and replayed with new inputs in the same tensors, eager work between the replays: each replay
+    gives the eager result bit for bit.  Two graphs have workspaces of their own."""
+    def state(seed):
+        x, dy, gamma, beta, s = gn_case((3, 9, 10, 24), seed, True)
+        c = adapter_case(mixed(70, 5, seed), 240, 36, 6, 5, seed)
+        return dict(x=dev(x), dy=dev(dy), gamma=dev(gamma), beta=dev(beta), skip=dev(s), rows=dev(c["rows"], np.int32), X=dev(c["X"]),
+                    base=dev(c["base"]), back=dev(c["back"]), dY=dev(c["dY"]), A=c["A"], B=c["B"], scale=dev(c["scale"]),
+                    p=dev(grads_of([1000], seed)[0]), q=dev(grads_of([37], seed)[0]))
+
+    def work(s):
+        y, mean, invstd = xb.gn_fwd(s["x"], s["gamma"], s["beta"], 6, 1e-5, xb.ACT_SILU, s["skip"])
+        grads = xb.gn_bwd(s["x"], s["dy"], s["gamma"], s["beta"], mean, invstd, xb.ACT_SILU, s["skip"])
+        plan = xb.adapter_plan(s["rows"], 5)
+        Y, T = xb.adapter_fwd(plan, s["base"], s["X"], s["A"], s["B"], s["scale"])
+        back = xb.adapter_bwd(plan, s["back"], s["dY"], s["X"], T, s["A"], s["B"], s["scale"])
+        p = [s["p"].clone(), s["q"].clone()]
+        norm = xb.clip_sgd(p, [s["p"], s["q"]], 0.1, 0.5)
+        clipped = [s["p"].clone(), s["q"].clone()]
+        xb.grad_clip(clipped, 0.25)
+        return [y, mean, invstd, *grads, Y, T, *back, *p, norm, *clipped, xb.grad_norm([s["dY"], s["X"]])]
+    fixed = [state(0), state(1)]
+    graphs, outs, side = [], [], torch.cuda.Stream()
+    for s in fixed:
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            work(s)
+        torch.cuda.current_stream().wait_stream(side)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            outs.append(work(s))
+        graphs.append(graph)
+    for turn in range(3):
+        for k in (0, 1):
+            new = state(10 + 2 * turn + k)
+            for name, t in fixed[k].items():
+                t.copy_(new[name])
+        want = [work(s) for s in fixed]
+        torch.cuda.synchronize()
+        for k in (1, 0):
+            graphs[k].replay()
+        torch.cuda.synchronize()
+        for k in (0, 1):
+            assert all(torch.equal(a, b) for a, b in zip(outs[k], want[k]))
