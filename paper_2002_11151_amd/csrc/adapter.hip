@@ -46,6 +46,7 @@ struct PlanAt {
   int* slot0;           // [adapters + 2]: first slot
   Entry* tiles;
   Entry* chunks;
+  int* rows;            // [tiles][kTileRows]: rows of a tile, the last one repeated: known without the tile's entry
 };
 constexpr int kMagic = 0x70ada37e;
 
@@ -74,6 +75,7 @@ inline size_t plan_layout(void* base, int M, int adapters, PlanAt* at) {
   l.slot0 = reinterpret_cast<int*>(take(((size_t)adapters + 2) * sizeof(int)));
   l.tiles = reinterpret_cast<Entry*>(take((size_t)max_tiles(M, adapters) * sizeof(Entry)));
   l.chunks = reinterpret_cast<Entry*>(take((size_t)max_chunks(M, adapters) * sizeof(Entry)));
+  l.rows = reinterpret_cast<int*>(take((size_t)max_tiles(M, adapters) * kTileRows * sizeof(int)));
   if (at) *at = l;
   return off;
 }
@@ -157,14 +159,22 @@ __global__ __launch_bounds__(256) void plan_place_kernel(const int32_t* rows, in
   if (bin > adapters) return;
   const int begin = p.start[bin], end = p.start[bin + 1], id = bin < adapters ? bin : -1, per_chunk = chunk_rows(M);
   if (begin == end) return;
-  int at = begin;
+  int at = begin, last = 0;
+  int* padded = p.rows + (size_t)p.tile0[bin] * kTileRows;
   for (int m0 = 0; m0 < M; m0 += 64) {
     const int m = m0 + lane;
     const bool mine = m < M && bin_of(rows[m], adapters) == bin;
     const unsigned long long all = __ballot(mine);
-    if (mine) p.perm[at + __popcll(all & ((1ull << lane) - 1))] = m;
+    if (mine) {
+      const int place = at + __popcll(all & ((1ull << lane) - 1));
+      p.perm[place] = m;
+      padded[place - begin] = m;
+    }
+    if (all) last = m0 + 63 - __clzll(all);
     at += __popcll(all);
   }
+  const int odd = (end - begin) % kTileRows;
+  if (odd && lane < kTileRows - odd) padded[end - begin + lane] = last;
   const int tiles = (end - begin + kTileRows - 1) / kTileRows;
   for (int i = lane; i < tiles; i += 64) {
     const int from = begin + i * kTileRows;
@@ -186,12 +196,16 @@ __device__ __forceinline__ bool planned(const PlanAt& p, int M, int adapters) {
 __device__ __forceinline__ float wide(float x) { return x; }
 __device__ __forceinline__ float wide(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }   // bfloat16
 
+// The base passes through once and should not take the caches' room.  (The output is stored the ordinary way: 4096 x 4096 values and a ReLU
+// that reads them take 57 us together, 62 if the output passes the caches by.)
+__device__ __forceinline__ f4 once4(const float* p) { return __builtin_nontemporal_load(reinterpret_cast<const f4*>(p)); }
+
 // Four values from p on, those at place k and beyond `end` zero; QUADS: all or none of the four are inside, and p is aligned.
-template <bool QUADS>
+template <bool QUADS, bool ONCE = false>
 __device__ __forceinline__ f4 load4(const float* p, int k, int end) {
   f4 v = {0.0f, 0.0f, 0.0f, 0.0f};
   if constexpr (QUADS) {
-    if (k < end) v = *reinterpret_cast<const f4*>(p);
+    if (k < end) v = ONCE ? once4(p) : *reinterpret_cast<const f4*>(p);
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -225,42 +239,87 @@ __device__ __forceinline__ void store4(float* p, f4 v, int k, int end) {
   }
 }
 
-// part[split][sorted row][16 RT] = X A^T over the split's share of K.  Block: one tile, its four waves side by side along K, joined in
-// LDS.  The instruction adds up over four k, one per quarter of the wave; a lane's 16-byte loads hold four neighbouring k of one row, so
-// the four instructions of a step take k = 4 (lane / 16) + j from both operands.  Rows beyond the tile and ranks beyond the last repeat a
-// valid one: their products are not stored.
-template <class T, bool QUADS, int RT>
-__global__ __launch_bounds__(256) void shrink_kernel(PlanAt plan, const float* X, const T* A, float* part, int M, int K, int rank, int adapters,
-                                                     int per_split) {
-  __shared__ float red[4][kTileRows][16 * RT];
-  if (!planned(plan, M, adapters) || (int)blockIdx.x >= plan.head[3]) return;
-  const Entry tile = plan.tiles[blockIdx.x];
-  if (tile.adapter < 0) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quarter = lane >> 4;
-  const bool two = tile.count > 16;
-  const float* x0 = X + (size_t)plan.perm[tile.begin + min(col, tile.count - 1)] * K;
-  const float* x1 = X + (size_t)plan.perm[tile.begin + min(col + 16, tile.count - 1)] * K;
-  const T* a[RT];
+// 4 x 4 transposition inside every four neighbouring lanes: register i of lane j goes to register j of lane i.  PERM: whose value a lane
+// takes; upper lanes take the other's b for their a, lower lanes the other's a for their b.
+template <int PERM>
+__device__ __forceinline__ void exchange(float& a, float& b, bool upper) {
+  const float from_a = __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(a), PERM, 0xF, 0xF, true));
+  const float from_b = __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(b), PERM, 0xF, 0xF, true));
+  a = upper ? from_b : a;
+  b = upper ? b : from_a;
+}
+__device__ __forceinline__ void quad_transpose(f4& v0, f4& v1, f4& v2, f4& v3, bool odd, bool high) {
 #pragma unroll
-  for (int t = 0; t < RT; ++t) a[t] = A + ((size_t)tile.adapter * rank + min(16 * t + col, rank - 1)) * K;
+  for (int e = 0; e < 4; ++e) {
+    float a = v0[e], b = v1[e], c = v2[e], d = v3[e];
+    exchange<0xB1>(a, b, odd);           // lanes 1 0 3 2
+    exchange<0xB1>(c, d, odd);
+    exchange<0x4E>(a, c, high);          // lanes 2 3 0 1
+    exchange<0x4E>(b, d, high);
+    v0[e] = a; v1[e] = b; v2[e] = c; v3[e] = d;
+  }
+}
+
+// part[split][sorted row][16 RT] = X A^T over the split's share of K.  Block: one tile, its four waves side by side along K, joined in
+// LDS.  A wave takes 64 k at a time.  The instruction wants lane = row + 16 slot, but loads in which neighbouring lanes lie in different
+// rows cost an access of the vector cache per lane (measured: 61 per load instead of 16); so lane 4 g + j of quarter q loads k =
+// 16 q + 4 j of row 4 g + i for i = 0 .. 3 (64 neighbouring bytes per four lanes), and a transposition inside the four lanes leaves every
+// lane with its own row: register s holds k = 16 q + 4 s, from both operands, so instruction (s, e) adds up k = 16 q + 4 s + e over the
+// quarters q.  Rows beyond the tile and ranks beyond the last repeat a valid one: their products are not stored.
+template <class T, bool QUADS, int RT>
+__global__ __launch_bounds__(256, RT == 1 ? 4 : RT == 2 ? 3 : RT == 4 ? 2 : 1) void shrink_kernel(PlanAt plan, const float* X, const T* A, float* part, int M, int K, int rank, int adapters,
+                                                     int splits, int per_split) {
+  __shared__ float red[4][kTileRows][16 * RT];
+  const int item = blockIdx.x / splits, split = blockIdx.x - item * splits;       // neighbouring blocks: the same rows
+  const Entry tile = plan.tiles[item];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quarter = lane >> 4;
+  const int four = col & ~3, ahead = 16 * quarter + 4 * (col & 3);
+  int row_of_tile[2][4];                                        // on its way with the entry
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) row_of_tile[h][i] = plan.rows[item * kTileRows + 16 * h + four + i];
+  if (!planned(plan, M, adapters) || item >= plan.head[3] || tile.adapter < 0) return;
+  const bool two = tile.count > 16, odd = lane & 1, high = lane & 2;
+  const float* x[2][4];
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[h][i] = X + (size_t)row_of_tile[h][i] * K + ahead;
+  const T* a = A + (size_t)tile.adapter * rank * K;
+  unsigned row[RT][4];
+#pragma unroll
+  for (int t = 0; t < RT; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) row[t][i] = (unsigned)min(16 * t + four + i, rank - 1) * (unsigned)K + ahead;
   f4 acc[2][RT];
 #pragma unroll
   for (int t = 0; t < RT; ++t) acc[0][t] = acc[1][t] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-  const int k0 = blockIdx.y * per_split, k1 = min(k0 + per_split, K);
-  for (int k = k0 + 16 * wave + 4 * quarter; k < k1 + 4 * quarter; k += 64) {      // the same number of steps for the whole wave
-    const f4 u = load4<QUADS>(x0 + k, k, k1);
-    f4 w = u;
-    if (two) w = load4<QUADS>(x1 + k, k, k1);
-    f4 b[RT];
+  const int k1 = min((split + 1) * per_split, K);
+  for (int k = split * per_split + 64 * wave; k < k1; k += 256) {
+    f4 u[4], w[4] = {}, b[RT][4];
 #pragma unroll
-    for (int t = 0; t < RT; ++t) b[t] = load4<QUADS>(a[t] + k, k, k1);
+    for (int i = 0; i < 4; ++i) u[i] = load4<QUADS>(x[0][i] + k, k + ahead, k1);
+    if (two)
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+      for (int i = 0; i < 4; ++i) w[i] = load4<QUADS>(x[1][i] + k, k + ahead, k1);
 #pragma unroll
-      for (int t = 0; t < RT; ++t) {
-        acc[0][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(u[j], b[t][j], acc[0][t], 0, 0, 0);
-        if (two) acc[1][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[j], b[t][j], acc[1][t], 0, 0, 0);
-      }
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) b[t][i] = load4<QUADS>(a + (row[t][i] + (unsigned)k), k + ahead, k1);
+    quad_transpose(u[0], u[1], u[2], u[3], odd, high);
+    if (two) quad_transpose(w[0], w[1], w[2], w[3], odd, high);
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      quad_transpose(b[t][0], b[t][1], b[t][2], b[t][3], odd, high);
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          acc[0][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(u[s][e], b[t][s][e], acc[0][t], 0, 0, 0);
+          if (two) acc[1][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[s][e], b[t][s][e], acc[1][t], 0, 0, 0);
+        }
+    }
   }
 #pragma unroll
   for (int h = 0; h < 2; ++h)
@@ -270,101 +329,188 @@ __global__ __launch_bounds__(256) void shrink_kernel(PlanAt plan, const float* X
       for (int i = 0; i < 4; ++i) red[wave][16 * h + 4 * quarter + i][16 * t + col] = acc[h][t][i];
   __syncthreads();
   for (int i = threadIdx.x; i < tile.count * 16 * RT; i += 256) {
-    const int row = i / (16 * RT), r = i - row * (16 * RT);
-    part[((size_t)blockIdx.y * M + tile.begin + row) * (16 * RT) + r] = (red[0][row][r] + red[1][row][r]) + (red[2][row][r] + red[3][row][r]);
+    const int row_of = i / (16 * RT), r = i - row_of * (16 * RT);
+    part[((size_t)split * M + tile.begin + row_of) * (16 * RT) + r] =
+        (red[0][row_of][r] + red[1][row_of][r]) + (red[2][row_of][r] + red[3][row_of][r]);
   }
 }
 
-// out = base + sum over ranks of scale (sum of the splits) B.  Block: one tile and 256 columns, a wave 64 of them; a lane's 16-byte
-// loads of B hold four neighbouring columns, one for each of four matrix tiles, so that base and out are touched 16 bytes wide too.
-// The blocks of the first columns also keep the sums (`kept`, times scale with KEEP_SCALED).
-template <class T, bool QUADS, int RT, bool KEEP_SCALED>
-__global__ __launch_bounds__(256) void expand_kernel(PlanAt plan, const float* base, const float* part, int splits, const float* scale, const T* B,
-                                                     float* out, float* kept, int M, int N, int rank, int adapters) {
+// Sum of `splits` values `each` apart, in their order, eight loads in flight.
+__device__ __forceinline__ float sum_of_splits(const float* part, size_t each, int splits) {
+  float s = 0.0f;
+  for (int k0 = 0; k0 < splits; k0 += 8) {
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = part[(size_t)min(k0 + k, splits - 1) * each];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s += k0 + k < splits ? v[k] : 0.0f;
+  }
+  return s;
+}
+
+// out = base + sum over ranks of scale (sum of the splits) B.  Block: one tile and `cols` columns.  A wave takes 16 rows and 64 columns at a
+// time: two waves the tile's halves and two column by column beside them, or all four side by side where the tile has up to 16 rows.
+// A lane's 16-byte loads of B hold four neighbouring columns, one for each of four matrix tiles, so that base and out are touched 16
+// bytes wide too; the first loads are on their way while the block adds up the splits.  The blocks of the first columns also keep the sums
+// (`kept`: in the rows' own order).
+template <class T, bool QUADS, int RT>
+__global__ __launch_bounds__(256, RT <= 2 ? 4 : 2) void expand_kernel(PlanAt plan, const float* base, const float* part, int splits, const float* scale, const T* B,
+                                                        float* out, float* kept, int M, int N, int rank, int adapters, int cols, int strips) {
   __shared__ float ts[kTileRows][16 * RT + 1];
-  if (!planned(plan, M, adapters) || (int)blockIdx.x >= plan.head[3]) return;
-  const Entry tile = plan.tiles[blockIdx.x];
+  const int item = blockIdx.x / strips, strip = blockIdx.x - item * strips;       // neighbouring blocks: the same rows
+  const Entry tile = plan.tiles[item];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quarter = lane >> 4;
-  const int n = blockIdx.y * 256 + 64 * wave + 4 * col;
+  int row_of_tile[2][4];                                        // on its way with the entry
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) row_of_tile[h][i] = plan.rows[item * kTileRows + 16 * h + 4 * quarter + i];
+  if (!planned(plan, M, adapters) || item >= plan.head[3]) return;
+  const int n1 = min((strip + 1) * cols, N);
   if (tile.adapter < 0) {                                      // rows without an adapter: as they were
-    if (out && out != base)
+    if (out != base)
       for (int i = quarter; i < tile.count; i += 4) {
-        const size_t at = (size_t)plan.perm[tile.begin + i] * N + n;
-        store4<QUADS>(out + at, load4<QUADS>(base + at, n, N), n, N);
+        const size_t at = (size_t)plan.perm[tile.begin + i] * N;
+        for (int n = strip * cols + 64 * wave + 4 * col; n < n1; n += 256)
+          store4<QUADS>(out + at + n, load4<QUADS, true>(base + at + n, n, n1), n, n1);
       }
-    if (blockIdx.y == 0 && kept)
+    if (strip == 0 && kept)
       for (int i = threadIdx.x; i < tile.count * rank; i += 256) kept[(size_t)plan.perm[tile.begin + i / rank] * rank + i % rank] = 0.0f;
     return;
   }
-  const float f = scale[tile.adapter];
+  const bool two = tile.count > 16;
+  const int half = two ? 16 * (wave & 1) : 0, beside = two ? 128 : 256;           // first row of the wave, columns of all waves
+  int n = strip * cols + 64 * (two ? wave >> 1 : wave);                           // of the wave; the lane's: + 4 col
+  size_t row_at[4];
+  bool in[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = half + 4 * quarter + i;
+    in[i] = row < tile.count;
+    row_at[i] = (size_t)(half ? row_of_tile[1][i] : row_of_tile[0][i]) * N + 4 * col;
+  }
+  const T* b = B + ((size_t)tile.adapter * rank + quarter) * N + 4 * col;
+  constexpr int STEPS = 4 * RT, U = STEPS < 8 ? STEPS : 8;       // steps of four ranks; U of them loaded at a time
+  f4 w[U], v[4];
+  auto load_w = [&](int s0) {
+#pragma unroll
+    for (int s = 0; s < U; ++s) w[s] = load4<QUADS>(b + (size_t)(4 * (s0 + s)) * N + n, n + 4 * col, 4 * (s0 + s) + quarter < rank ? n1 : 0);
+  };
+  auto load_v = [&]() {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = load4<QUADS, true>(base + row_at[i] + n, n + 4 * col, in[i] ? n1 : 0);
+  };
+  load_v();
+  load_w(0);
+  const float f = scale ? scale[tile.adapter] : 1.0f;
   for (int i = threadIdx.x; i < kTileRows * 16 * RT; i += 256) {
     const int row = i / (16 * RT), r = i - row * (16 * RT);
     float s = 0.0f;
     if (row < tile.count && r < rank) {
-      for (int k = 0; k < splits; ++k) s += part[((size_t)k * M + tile.begin + row) * (16 * RT) + r];
-      if (blockIdx.y == 0 && kept) kept[(size_t)plan.perm[tile.begin + row] * rank + r] = KEEP_SCALED ? f * s : s;
+      s = sum_of_splits(part + (size_t)(tile.begin + row) * (16 * RT) + r, (size_t)M * 16 * RT, splits);
+      if (strip == 0 && kept) kept[(size_t)plan.perm[tile.begin + row] * rank + r] = s;
       s *= f;
     }
     ts[row][r] = s;
   }
   __syncthreads();
-  if (!out) return;
-  f4 acc[2][4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) acc[0][e] = acc[1][e] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-  const T* b = B + (size_t)tile.adapter * rank * N + n;
-  const int steps = (rank + 3) / 4;
-  for (int s = 0; s < steps; ++s) {
-    const int r = 4 * s + quarter;
-    const f4 w = load4<QUADS>(b + (size_t)r * N, n, r < rank ? N : 0);
-    const float u = ts[col][r], v = ts[col + 16][r];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      acc[0][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(u, w[e], acc[0][e], 0, 0, 0);
-      acc[1][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, w[e], acc[1][e], 0, 0, 0);
+  for (bool first = true; n < n1; n += beside, first = false) {
+    if (!first) {
+      load_v();
+      load_w(0);
     }
-  }
+    f4 acc[4];
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
+    for (int e = 0; e < 4; ++e) acc[e] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+    for (int s0 = 0; s0 < STEPS; s0 += U) {
+      if (s0) load_w(s0);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int row = 16 * h + 4 * quarter + i;
-      if (row < tile.count) {
-        const size_t at = (size_t)plan.perm[tile.begin + row] * N + n;
-        f4 v = load4<QUADS>(base + at, n, N);
+      for (int s = 0; s < U; ++s) {
+        const float t = ts[half + col][4 * (s0 + s) + quarter];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] += acc[h][e][i];
-        store4<QUADS>(out + at, v, n, N);
+        for (int e = 0; e < 4; ++e) acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(t, w[s][e], acc[e], 0, 0, 0);
       }
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[i][e] += acc[e][i];
+      store4<QUADS>(out + row_at[i] + n, v[i], n + 4 * col, in[i] ? n1 : 0);
+    }
+  }
 }
 
-// grad[adapter][r][k] = scale sum_m S[m][r] X[m][k] over a chunk's rows: into the gradient where the adapter has no other chunk, else into
-// the chunk's slot.  The instruction adds up over four rows, one per quarter of the wave.
+// sum[sorted row][16 RT] = scale times the sum of the splits, zero beyond the last rank.
+template <int RT>
+__global__ __launch_bounds__(256) void split_sum_kernel(PlanAt plan, const float* part, int splits, const float* scale, float* sum, int M, int rank,
+                                                        int adapters) {
+  const Entry tile = plan.tiles[blockIdx.x];
+  if (!planned(plan, M, adapters) || (int)blockIdx.x >= plan.head[3] || tile.adapter < 0) return;
+  const int i = blockIdx.y * 256 + threadIdx.x;
+  if (i >= tile.count * 16 * RT) return;
+  const size_t at = (size_t)tile.begin * 16 * RT + i;
+  sum[at] = i % (16 * RT) < rank ? scale[tile.adapter] * sum_of_splits(part + at, (size_t)M * 16 * RT, splits) : 0.0f;
+}
+
+struct Outer {
+  const float *S, *X;       // S: [row][rank], or [sorted row][stride] with `sorted`
+  float *grad, *slots;
+  int K, strips, stride, sorted;
+};
+
+// grad[adapter][r][k] = f sum_m S[m][r] X[m][k] over a chunk's rows: into the gradient where the adapter has no other chunk, else into
+// the chunk's slot.  Block: 64 columns; its four waves take every fourth step of four rows each and are joined in LDS, two and two.  The
+// instruction adds up over four rows, one per quarter of the wave.  A wave's loads of eight steps are in flight together.
 template <bool QUADS, int RT>
-__device__ __forceinline__ void outer_of(const PlanAt& plan, const Entry& chunk, int strip, const float* S, const float* X, float f, float* grad,
-                                         float* slots, int K, int rank) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quarter = lane >> 4;
-  const int k = strip * 256 + 64 * wave + 4 * col;
-  if (strip * 256 + 64 * wave >= K) return;
+__device__ __forceinline__ void outer_of(const PlanAt& plan, const Entry& chunk, int strip, const Outer& o, float f, int rank, f4 (&red)[2][RT][4][64]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quarter = lane >> 4, K = o.K;
+  const int k = strip * 64 + 4 * col;
   f4 acc[RT][4];
 #pragma unroll
   for (int t = 0; t < RT; ++t)
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[t][e] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-  for (int i = 0; i < chunk.count; i += 4) {
-    const bool in = i + quarter < chunk.count;
-    const size_t m = (size_t)plan.perm[chunk.begin + min(i + quarter, chunk.count - 1)];
-    const f4 x = load4<QUADS>(X + m * K + k, k, in ? K : 0);
-    float s[RT];
+  constexpr int U = RT <= 2 ? 8 : RT == 4 ? 4 : 2;
+  for (int i0 = 4 * wave; i0 < chunk.count; i0 += 16 * U) {
+    int m[U];
+    f4 x[U];
+    float s[U][RT];
 #pragma unroll
-    for (int t = 0; t < RT; ++t) s[t] = in ? S[m * rank + min(16 * t + col, rank - 1)] : 0.0f;
+    for (int u = 0; u < U; ++u) m[u] = plan.perm[chunk.begin + min(i0 + 16 * u + quarter, chunk.count - 1)];
 #pragma unroll
-    for (int t = 0; t < RT; ++t)
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + 16 * u + quarter;
+      const bool in = i < chunk.count;
+      x[u] = load4<QUADS>(o.X + (size_t)m[u] * K + k, k, in ? K : 0);
+      const float* from = o.S + (o.sorted ? (size_t)(chunk.begin + min(i, chunk.count - 1)) : (size_t)m[u]) * o.stride;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[t][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(s[t], x[e], acc[t][e], 0, 0, 0);
+      for (int t = 0; t < RT; ++t) s[u][t] = in ? from[min(16 * t + col, rank - 1)] : 0.0f;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (i0 + 16 * u < chunk.count)                           // the wave's first row of the step
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[t][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(s[u][t], x[u][e], acc[t][e], 0, 0, 0);
   }
-  float* to = chunk.slot < 0 ? grad + (size_t)chunk.adapter * rank * K : slots + (size_t)chunk.slot * rank * K;
+  for (int half = 2; half; half >>= 1) {                      // waves 2 and 3 to 0 and 1, then 1 to 0
+    if (half == 1) __syncthreads();
+    if (wave >= half && wave < 2 * half)
+#pragma unroll
+      for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) red[wave - half][t][e][lane] = acc[t][e];
+    __syncthreads();
+    if (wave < half)
+#pragma unroll
+      for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[t][e] += red[wave][t][e][lane];
+  }
+  if (wave) return;
+  float* to = chunk.slot < 0 ? o.grad + (size_t)chunk.adapter * rank * K : o.slots + (size_t)chunk.slot * rank * K;
 #pragma unroll
   for (int t = 0; t < RT; ++t)
 #pragma unroll
@@ -374,34 +520,49 @@ __device__ __forceinline__ void outer_of(const PlanAt& plan, const Entry& chunk,
     }
 }
 
-struct Outer {
-  const float *S, *X;       // S: [row][rank]
-  float *grad, *slots;
-  int K, strips;
-};
-
-// Both gradients in one launch: the first strips are dA's (S = dT), the others dB's (S = T, times scale).
+// Both gradients in one launch: the first strips are dA's (S = dT), the others dB's (S = T, times scale); behind the chunks a strip's
+// blocks, `zeros` of them, clear the gradients of adapters without rows.
 template <bool QUADS, int RT>
-__global__ __launch_bounds__(256) void outer_kernel(PlanAt plan, Outer a, Outer b, const float* scale, int M, int rank, int adapters) {
-  if (!planned(plan, M, adapters) || (int)blockIdx.x >= plan.head[4]) return;
-  const Entry chunk = plan.chunks[blockIdx.x];
-  if ((int)blockIdx.y < a.strips) outer_of<QUADS, RT>(plan, chunk, blockIdx.y, a.S, a.X, 1.0f, a.grad, a.slots, a.K, rank);
-  else outer_of<QUADS, RT>(plan, chunk, blockIdx.y - a.strips, b.S, b.X, scale[chunk.adapter], b.grad, b.slots, b.K, rank);
+__global__ __launch_bounds__(256) void outer_kernel(PlanAt plan, Outer a, Outer b, const float* scale, int M, int rank, int adapters, int chunks,
+                                                    int zeros) {
+  __shared__ f4 red[2][RT][4][64];
+  const int item = blockIdx.x / (a.strips + b.strips), strip = blockIdx.x - item * (a.strips + b.strips);
+  if (item >= chunks) {
+    if (!planned(plan, M, adapters)) return;
+    const Outer& o = strip < a.strips ? a : b;
+    const int k = (strip < a.strips ? strip : strip - a.strips) * 64 + (threadIdx.x & 63);
+    if (k >= o.K) return;
+    for (int id = item - chunks; id < adapters; id += zeros)
+      if (plan.chunk0[id] == plan.chunk0[id + 1])
+        for (int r = threadIdx.x >> 6; r < rank; r += 4) o.grad[((size_t)id * rank + r) * o.K + k] = 0.0f;
+    return;
+  }
+  const Entry chunk = plan.chunks[item];
+  if (!planned(plan, M, adapters) || item >= plan.head[4]) return;
+  if (strip < a.strips) outer_of<QUADS, RT>(plan, chunk, strip, a, 1.0f, rank, red);
+  else outer_of<QUADS, RT>(plan, chunk, strip - a.strips, b, scale[chunk.adapter], rank, red);
 }
 
-// Gradients of adapters with several chunks, or with none.
+// Gradients of adapters with several chunks; VEC values per thread.
+template <int VEC>
 __global__ __launch_bounds__(256) void outer_join_kernel(PlanAt plan, Outer a, Outer b, int M, int rank, int adapters) {
   if (!planned(plan, M, adapters)) return;
   const int id = blockIdx.x, chunks = plan.chunk0[id + 1] - plan.chunk0[id];
-  if (chunks == 1) return;
+  if (chunks < 2) return;
   const int slot = plan.slot0[id];
   for (int h = 0; h < 2; ++h) {
     const Outer& o = h ? b : a;
     const size_t each = (size_t)rank * o.K;
-    for (size_t i = (size_t)blockIdx.y * 256 + threadIdx.x; i < each; i += (size_t)gridDim.y * 256) {
-      float s = 0.0f;
-      for (int k = 0; k < chunks; ++k) s += o.slots[(size_t)(slot + k) * each + i];
-      o.grad[(size_t)id * each + i] = s;
+    for (size_t i = ((size_t)blockIdx.y * 256 + threadIdx.x) * VEC; i < each; i += (size_t)gridDim.y * 256 * VEC) {
+      f4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+      for (int k0 = 0; k0 < chunks; k0 += 8) {                // eight loads in flight, added in their order
+        f4 v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = load4<VEC == 4>(o.slots + (size_t)(slot + min(k0 + k, chunks - 1)) * each + i, 0, k0 + k < chunks ? VEC : 0);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s += v[k];
+      }
+      store4<VEC == 4>(o.grad + (size_t)id * each + i, s, 0, VEC);
     }
   }
 }
@@ -409,22 +570,32 @@ __global__ __launch_bounds__(256) void outer_join_kernel(PlanAt plan, Outer a, O
 // ---- launches --------------------------------------------------------------------------------------
 inline int rank_tiles(int rank) { return rank <= 16 ? 1 : rank <= 32 ? 2 : rank <= 64 ? 4 : 8; }
 
-// Shares of K: about 1024 blocks, at least one step of all four waves each, 32 at most (their sums are read by every block of columns).
+// Shares of K: about 1024 blocks, at least 64 k for each of the four waves, 16 at most (every block of columns adds them up again).
 struct Split {
   int splits, per_split;
   Split(int M, int K, int adapters) {
     const long long tiles = max_tiles(M, adapters);
-    const int wanted = (int)std::max<long long>(1, std::min<long long>(32, 1024 / tiles));
-    per_split = std::max(64, ((K + wanted - 1) / wanted + 63) / 64 * 64);
+    const int wanted = (int)std::max<long long>(1, std::min<long long>(16, 1024 / tiles));
+    per_split = ((K + wanted - 1) / wanted + 255) / 256 * 256;
     splits = (K + per_split - 1) / per_split;
   }
 };
 
+// Columns of a block of expand_kernel: 1024 where that leaves about 1024 blocks, else fewer, 256 at least.
+inline int columns(int M, int N, int adapters) {
+  int cols = 1024;
+  while (cols > 256 && max_tiles(M, adapters) * ((N + cols - 1) / cols) < 1024) cols >>= 1;
+  return cols;
+}
+
 int shape_ok(int M, int K, int N, int rank, int adapters) {
   if (M <= 0 || K <= 0 || N <= 0 || rank <= 0 || adapters <= 0 || rank > kMaxRank) return XBAR_ESHAPE;
   if (M > (1 << 24) || K >= (1 << 24) || N >= (1 << 24) || adapters > 65536) return XBAR_ESHAPE;
-  if ((double)M * std::max(K, N) >= 274877906944.0 || (double)adapters * rank * std::max(K, N) >= 274877906944.0) return XBAR_ESHAPE;
-  return XBAR_OK;
+  const double wide = std::max(K, N);
+  if (M * wide >= 274877906944.0 || adapters * rank * wide >= 274877906944.0 || rank * wide >= 1073741824.0) return XBAR_ESHAPE;
+  // blocks of a launch: below 2^24 (a launch has fewer than 2^32 threads)
+  const double most = std::max(max_tiles(M, adapters) * std::max(16.0, (wide + 255) / 256), (max_chunks(M, adapters) + 4) * ((double)K + N + 126) / 64);
+  return most >= 16777216.0 ? XBAR_ESHAPE : XBAR_OK;
 }
 
 struct WorkAt {
@@ -441,7 +612,7 @@ size_t work_layout(void* ws, int op, int M, int K, int N, int rank, int adapters
   WorkAt w{};
   w.part = take((size_t)Split(M, op == XBAR_OP_FWD ? K : N, adapters).splits * M * 16 * rank_tiles(rank));
   if (op == XBAR_OP_BWD) {
-    w.dT = take((size_t)M * rank);
+    w.dT = take((size_t)M * 16 * rank_tiles(rank));
     w.slotsA = take((size_t)max_slots(M) * rank * K);
     w.slotsB = take((size_t)max_slots(M) * rank * N);
   }
@@ -453,20 +624,25 @@ size_t work_layout(void* ws, int op, int M, int K, int N, int rank, int adapters
 template <class T, bool QUADS, int RT>
 struct Kernels {
   static int shrink(const PlanAt& plan, const float* X, const void* A, float* part, int M, int K, int rank, int adapters, const Split& s, hipStream_t st) {
-    hipLaunchKernelGGL((shrink_kernel<T, QUADS, RT>), dim3((unsigned)max_tiles(M, adapters), (unsigned)s.splits), dim3(256), 0, st, plan, X,
-                       reinterpret_cast<const T*>(A), part, M, K, rank, adapters, s.per_split);
+    hipLaunchKernelGGL((shrink_kernel<T, QUADS, RT>), dim3((unsigned)(max_tiles(M, adapters) * s.splits)), dim3(256), 0, st, plan, X,
+                       reinterpret_cast<const T*>(A), part, M, K, rank, adapters, s.splits, s.per_split);
     return launched();
   }
-  template <bool KEEP_SCALED>
   static int expand(const PlanAt& plan, const float* base, const float* part, int splits, const float* scale, const void* B, float* out, float* kept,
                     int M, int N, int rank, int adapters, hipStream_t st) {
-    hipLaunchKernelGGL((expand_kernel<T, QUADS, RT, KEEP_SCALED>), dim3((unsigned)max_tiles(M, adapters), out ? (unsigned)((N + 255) / 256) : 1u),
-                       dim3(256), 0, st, plan, base, part, splits, scale, reinterpret_cast<const T*>(B), out, kept, M, N, rank, adapters);
+    const int cols = columns(M, N, adapters), strips = (N + cols - 1) / cols;
+    hipLaunchKernelGGL((expand_kernel<T, QUADS, RT>), dim3((unsigned)(max_tiles(M, adapters) * strips)), dim3(256), 0, st, plan, base, part, splits,
+                       scale, reinterpret_cast<const T*>(B), out, kept, M, N, rank, adapters, cols, strips);
+    return launched();
+  }
+  static int split_sum(const PlanAt& plan, const float* part, int splits, const float* scale, float* sum, int M, int rank, int adapters, hipStream_t st) {
+    hipLaunchKernelGGL(split_sum_kernel<RT>, dim3((unsigned)max_tiles(M, adapters), 2 * RT), dim3(256), 0, st, plan, part, splits, scale, sum, M, rank, adapters);
     return launched();
   }
   static int outer(const PlanAt& plan, const Outer& a, const Outer& b, const float* scale, int M, int rank, int adapters, hipStream_t st) {
-    hipLaunchKernelGGL((outer_kernel<QUADS, RT>), dim3((unsigned)max_chunks(M, adapters), (unsigned)(a.strips + b.strips)), dim3(256), 0, st, plan, a,
-                       b, scale, M, rank, adapters);
+    const int chunks = (int)max_chunks(M, adapters), zeros = std::min(adapters, 4);
+    hipLaunchKernelGGL((outer_kernel<QUADS, RT>), dim3((unsigned)((chunks + zeros) * (a.strips + b.strips))), dim3(256), 0, st, plan, a, b, scale, M,
+                       rank, adapters, chunks, zeros);
     return launched();
   }
 };
@@ -537,7 +713,7 @@ int xbar_adapter_fwd(const void* plan, size_t plan_bytes, const float* base, con
   const int rc = with_kernels(type, K % 4 == 0, rank, [&](auto k) { return k.shrink(p, X, A, w.part, M, K, rank, adapters, s, st); });
   if (rc) return rc;
   return with_kernels(type, N % 4 == 0, rank, [&](auto k) {
-    return k.template expand<false>(p, base, w.part, s.splits, scale, B, Y, T, M, N, rank, adapters, st);
+    return k.expand(p, base, w.part, s.splits, scale, B, Y, T, M, N, rank, adapters, st);
   });
 }
 
@@ -568,16 +744,21 @@ int xbar_adapter_bwd(const void* plan, size_t plan_bytes, const float* base, con
   const Split s(M, N, adapters);
   int rc = with_kernels(type, N % 4 == 0, rank, [&](auto k) { return k.shrink(p, dY, B, w.part, M, N, rank, adapters, s, st); });
   if (rc) return rc;
-  rc = with_kernels(type, K % 4 == 0, rank, [&](auto k) {
-    return k.template expand<true>(p, base, w.part, s.splits, scale, A, dX, w.dT, M, K, rank, adapters, st);
-  });
+  rc = with_kernels(XBAR_F32, true, rank, [&](auto k) { return k.split_sum(p, w.part, s.splits, scale, w.dT, M, rank, adapters, st); });
   if (rc) return rc;
-  const Outer oa{w.dT, X, dA, w.slotsA, K, (K + 255) / 256}, ob{T, dY, dB, w.slotsB, N, (N + 255) / 256};
+  if (dX) {
+    rc = with_kernels(type, K % 4 == 0, rank,
+                      [&](auto k) { return k.expand(p, base, w.dT, 1, (const float*)nullptr, A, dX, (float*)nullptr, M, K, rank, adapters, st); });
+    if (rc) return rc;
+  }
+  const Outer oa{w.dT, X, dA, w.slotsA, K, (K + 63) / 64, 16 * rank_tiles(rank), 1}, ob{T, dY, dB, w.slotsB, N, (N + 63) / 64, rank, 0};
   rc = with_kernels(XBAR_F32, K % 4 == 0 && N % 4 == 0, rank, [&](auto k) { return k.outer(p, oa, ob, scale, M, rank, adapters, st); });
   if (rc) return rc;
-  const size_t most = (size_t)rank * std::max(K, N);
-  hipLaunchKernelGGL(outer_join_kernel, dim3((unsigned)adapters, (unsigned)std::min<size_t>(64, (most + 1023) / 1024)), dim3(256), 0, st, p, oa, ob, M,
-                     rank, adapters);
+  if (M <= chunk_rows(M)) return XBAR_OK;                       // no adapter has two chunks
+  const bool quads = (size_t)rank * K % 4 == 0 && (size_t)rank * N % 4 == 0;
+  const size_t most = (size_t)rank * std::max(K, N) / (quads ? 4 : 1);
+  hipLaunchKernelGGL(quads ? outer_join_kernel<4> : outer_join_kernel<1>, dim3((unsigned)adapters, (unsigned)std::min<size_t>(256, (most + 255) / 256)),
+                     dim3(256), 0, st, p, oa, ob, M, rank, adapters);
   return launched();
 }
 
