@@ -20,19 +20,26 @@ inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   return a && b && p < q + nb && q < p + na;
 }
 
-// VEC consecutive floats of memory (one, or four from a 16-byte boundary).
+// VEC consecutive floats of memory, from a boundary of as many.
 template <int VEC>
 __device__ __forceinline__ void load_vec(const float* p, float (&v)[VEC]) {
   if constexpr (VEC == 4) {
     const float4 q = *reinterpret_cast<const float4*>(p);
     v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+  } else if constexpr (VEC == 2) {
+    const float2 q = *reinterpret_cast<const float2*>(p);
+    v[0] = q.x; v[1] = q.y;
   } else {
     v[0] = *p;
   }
 }
-template <int VEC>
+// PAST: past the caches.
+template <int VEC, bool PAST = false>
 __device__ __forceinline__ void store_vec(float* p, const float (&v)[VEC]) {
-  if constexpr (VEC == 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+  typedef float f4 __attribute__((ext_vector_type(4)));
+  if constexpr (VEC == 4 && PAST) __builtin_nontemporal_store(f4{v[0], v[1], v[2], v[3]}, reinterpret_cast<f4*>(p));
+  else if constexpr (VEC == 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+  else if constexpr (VEC == 2) *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]);
   else *p = v[0];
 }
 
@@ -61,12 +68,33 @@ struct Shape {
   int chunks;                                             // blocks along a sample's positions
 };
 
-// A channel's normalisation in one sample.
+// A channel's normalisation in one sample: gamma (x - mean) invstd + beta = a x + b.  a is exact (a product of two floats), b rounded once, z
+// once more: the digits of a double, whatever the mean, for one conversion and one operation.
 struct Norm {
-  double gamma, beta, mean, invstd;
-  __device__ __forceinline__ double xhat(float x) const { return ((double)x - mean) * invstd; }
-  __device__ __forceinline__ double z(double xh) const { return __builtin_fma(gamma, xh, beta); }
+  double a, b;
+  __device__ __forceinline__ Norm() {}
+  __device__ __forceinline__ Norm(float gamma, float beta, float mean, float invstd) {
+    a = (double)gamma * (double)invstd;
+    b = __builtin_fma(-(double)mean, a, (double)beta);
+  }
+  __device__ __forceinline__ double z(float x) const { return __builtin_fma((double)x, a, b); }
 };
+// dx = invstd (gamma g - m0 - xhat m1), m0 and m1 the means over the group of gamma g and gamma g xhat: p g + q x + r.
+struct Slope {
+  double p, q, r;
+  __device__ __forceinline__ Slope() {}
+  __device__ __forceinline__ Slope(float gamma, float mean, float invstd, double m0, double m1) {
+    const double is = (double)invstd;
+    p = is * (double)gamma;
+    q = -is * is * m1;
+    r = __builtin_fma(-q, (double)mean, -is * m0);
+  }
+  __device__ __forceinline__ float dx(float g, float x) const { return (float)__builtin_fma((double)g, p, __builtin_fma((double)x, q, r)); }
+};
+// Sum of g xhat from those of g and of g x.
+__device__ __forceinline__ double xhat_sum(double g, double gx, float mean, float invstd) {
+  return (double)invstd * __builtin_fma(-(double)mean, g, gx);
+}
 
 template <int VEC>
 __device__ __forceinline__ void load_norm(Norm (&nm)[VEC], const Shape& s, int b, int c, const float* gamma, const float* beta,
@@ -74,10 +102,260 @@ __device__ __forceinline__ void load_norm(Norm (&nm)[VEC], const Shape& s, int b
 #pragma unroll
   for (int e = 0; e < VEC; ++e) {
     const int g = b * s.groups + (c + e) / s.per_group;
-    nm[e] = Norm{(double)gamma[c + e], (double)beta[c + e], (double)mean[g], (double)invstd[g]};
+    nm[e] = Norm(gamma[c + e], beta[c + e], mean[g], invstd[g]);
   }
 }
 
+// ---- a group held in registers ---------------------------------------------------------------------
+// TEAM threads keep all values of one sample's group, N vectors of VEC neighbouring channels each: memory is touched once in each
+// direction and one launch does it all.  Element i of the group is vector i % q of position i / q (q vectors per position).
+constexpr int team_block(int team) { return team < 256 ? 256 : team; }
+constexpr int kXcds = 8;
+
+// The team's group.  Blocks go round the eight chiplets, which have caches of their own: every chiplet gets neighbouring groups, which share
+// cache lines where a group's channels do not fill them.
+template <int TEAM>
+__device__ __forceinline__ int team_item() {
+  const int each = gridDim.x / kXcds, block = (blockIdx.x % kXcds) * each + blockIdx.x / kXcds;
+  return block * (team_block(TEAM) / TEAM) + threadIdx.x / TEAM;
+}
+
+// Places of a thread's elements: its next one is TEAM elements on.
+struct Walk {
+  int row, c, dr, dc, q;
+  __device__ __forceinline__ Walk(int t, int team, int vectors) : q(vectors) {
+    row = t / q;
+    c = t - row * q;
+    dr = team / q;
+    dc = team - dr * q;
+  }
+  __device__ __forceinline__ void next() {
+    row += dr;
+    c += dc;
+    if (c >= q) {
+      c -= q;
+      ++row;
+    }
+  }
+};
+
+// Sums over the team, the same bits in all of its threads; red: shared, for teams of several waves.
+template <int TEAM>
+__device__ __forceinline__ void team_sum(double& a, double& b, double (&red)[2][team_block(TEAM) / 64]) {
+#pragma unroll
+  for (int d = (TEAM < 64 ? TEAM : 64) / 2; d; d >>= 1) {
+    a += __shfl_xor(a, d, 64);
+    b += __shfl_xor(b, d, 64);
+  }
+  if constexpr (TEAM > 64) {
+    constexpr int W = TEAM / 64;
+    const int wave = threadIdx.x / 64, first = wave / W * W;
+    if ((threadIdx.x & 63) == 0) {
+      red[0][wave] = a;
+      red[1][wave] = b;
+    }
+    __syncthreads();
+    a = b = 0.0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      a += red[0][first + w];
+      b += red[1][first + w];
+    }
+  }
+}
+
+template <int ACT, int VEC, int TEAM, int N>
+__global__ __launch_bounds__(team_block(TEAM)) void gn_held_fwd_kernel(const float* x, const float* gamma, const float* beta, const float* skip,
+                                                                       float* y, float* mean, float* invstd, Shape s, float eps) {
+  __shared__ double red[2][team_block(TEAM) / 64];
+  const int item = team_item<TEAM>();
+  const bool mine = item < s.batch * s.groups;
+  const int b = mine ? item / s.groups : 0, g = mine ? item - b * s.groups : 0, q = s.per_group / VEC;
+  const int count = mine ? s.positions * q : 0, t = threadIdx.x % TEAM, c0 = g * s.per_group;
+  const size_t from = (size_t)b * s.positions * s.channels + c0;
+  float v[N][VEC];
+  {
+    Walk at(t, TEAM, q);
+#pragma unroll
+    for (int j = 0; j < N; ++j, at.next())
+      if (t + TEAM * j < count) load_vec<VEC>(x + from + (size_t)at.row * s.channels + at.c * VEC, v[j]);
+  }
+  const double x0 = mine ? (double)x[from] : 0.0;             // sums about the group's first value keep the digits of a small spread
+  double s0 = 0.0, s1 = 0.0;
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    if (t + TEAM * j < count)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        const double u = (double)v[j][e] - x0;
+        s0 += u;
+        s1 = __builtin_fma(u, u, s1);
+      }
+  team_sum<TEAM>(s0, s1, red);
+  const double n = (double)s.positions * s.per_group, m = s0 / n, var = s1 / n - m * m;
+  const float mu = (float)(x0 + m), is = (float)(1.0 / ::sqrt((var < 0.0 ? 0.0 : var) + (double)eps));
+  if (mine && t == 0) {
+    mean[item] = mu;
+    invstd[item] = is;
+  }
+  Walk at(t, TEAM, q);
+#pragma unroll
+  for (int j = 0; j < N; ++j, at.next())
+    if (t + TEAM * j < count) {
+      const size_t to = from + (size_t)at.row * s.channels + at.c * VEC;
+      float ga[VEC], be[VEC], k[VEC], o[VEC];
+      load_vec<VEC>(gamma + c0 + at.c * VEC, ga);
+      load_vec<VEC>(beta + c0 + at.c * VEC, be);
+      if (skip) load_vec<VEC>(skip + to, k);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        double z = Norm(ga[e], be[e], mu, is).z(v[j][e]);
+        if (skip) z += (double)k[e];
+        o[e] = act_of<ACT>(z);
+      }
+      store_vec<VEC>(y + to, o);
+    }
+}
+
+// Backward: q divides TEAM, so that a thread's elements all lie in the same channels.  sums[sample][channel][2]: sums of g and of g xhat over the
+// positions; with one sample they are dbeta and dgamma themselves and go there.
+template <int ACT, int VEC, int TEAM, int N>
+__global__ __launch_bounds__(team_block(TEAM)) void gn_held_bwd_kernel(const float* x, const float* dy, const float* gamma, const float* beta,
+                                                                       const float* skip, const float* mean, const float* invstd, float* dx,
+                                                                       float* dskip, double* sums, float* dgamma, float* dbeta, Shape s) {
+  constexpr int BLOCK = team_block(TEAM), WAVE = TEAM < 64 ? TEAM : 64, VALUES = 2 * VEC;
+  __shared__ double red[2][BLOCK / 64];
+  __shared__ double channel[VALUES * BLOCK];
+  const int item = team_item<TEAM>();
+  const bool mine = item < s.batch * s.groups;
+  const int b = mine ? item / s.groups : 0, g = mine ? item - b * s.groups : 0, q = s.per_group / VEC;
+  const int count = mine ? s.positions * q : 0, t = threadIdx.x % TEAM, row = t / q, c = t - row * q, dr = TEAM / q;
+  const int c0 = g * s.per_group;
+  const size_t from = (size_t)b * s.positions * s.channels + (size_t)row * s.channels + c0 + c * VEC, step = (size_t)dr * s.channels;
+  float v[N][VEC], d[N][VEC];
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    if (t + TEAM * j < count) {
+      load_vec<VEC>(x + from + j * step, v[j]);
+      load_vec<VEC>(dy + from + j * step, d[j]);
+    }
+  float ga[VEC], be[VEC];
+  load_vec<VEC>(gamma + c0 + c * VEC, ga);
+  load_vec<VEC>(beta + c0 + c * VEC, be);
+  const float mu = mine ? mean[item] : 0.0f, is = mine ? invstd[item] : 0.0f;
+  Norm nm[VEC];
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) nm[e] = Norm(ga[e], be[e], mu, is);
+  double p[VALUES];                                            // p[2 e]: sum of g, p[2 e + 1]: of g x
+#pragma unroll
+  for (int i = 0; i < VALUES; ++i) p[i] = 0.0;
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    if (t + TEAM * j < count) {
+      float k[VEC];
+      if (ACT != XBAR_ACT_NONE && skip) load_vec<VEC>(skip + from + j * step, k);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        double z = nm[e].z(v[j][e]);
+        if (ACT != XBAR_ACT_NONE && skip) z += (double)k[e];
+        d[j][e] = act_bwd<ACT>(z, d[j][e]);
+        p[2 * e] += (double)d[j][e];
+        p[2 * e + 1] = __builtin_fma((double)d[j][e], (double)v[j][e], p[2 * e + 1]);
+      }
+    }
+  // Over the lanes with the same channels: every level exchanges half of what is left and keeps the other half, so that a lane ends up with
+  // VALUES >> levels of the sums (or one, which several hold).
+  int left = VALUES, which = 0;
+#pragma unroll
+  for (int level = 0, dist = WAVE / 2; dist; ++level, dist >>= 1) {
+    if (dist >= q) {
+      const int half = (VALUES >> level) / 2;
+      if (half) {
+        const bool upper = t & dist;
+#pragma unroll
+        for (int i = 0; i < half; ++i) {
+          const double send = upper ? p[i] : p[i + half], keep = upper ? p[i + half] : p[i];
+          p[i] = keep + __shfl_xor(send, dist, 64);
+        }
+        which += upper ? half : 0;
+        left = half;
+      } else {
+        p[0] += __shfl_xor(p[0], dist, 64);
+      }
+    }
+  }
+  const int slots = q < WAVE ? TEAM / WAVE : dr, slot = q < WAVE ? t / WAVE : row;      // partial sums of a channel
+  double* shared = channel + (threadIdx.x / TEAM) * (VALUES * TEAM);
+#pragma unroll
+  for (int i = 0; i < VALUES; ++i)
+    if (i < left) shared[(slot * q + c) * VALUES + which + i] = p[i];
+  __syncthreads();
+  double s0 = 0.0, s1 = 0.0;
+  for (int i = t; i < s.per_group; i += TEAM) {
+    double sg = 0.0, sgx = 0.0;
+    for (int k = 0; k < slots; ++k) {
+      sg += shared[(k * s.per_group + i) * 2];
+      sgx += shared[(k * s.per_group + i) * 2 + 1];
+    }
+    sgx = xhat_sum(sg, sgx, mu, is);
+    const double f = (double)gamma[c0 + i];
+    s0 = __builtin_fma(f, sg, s0);
+    s1 = __builtin_fma(f, sgx, s1);
+    if (mine && s.batch > 1) {
+      double* to = sums + ((size_t)b * s.channels + c0 + i) * 2;
+      to[0] = sg;
+      to[1] = sgx;
+    } else if (mine) {
+      dbeta[c0 + i] = (float)sg;
+      dgamma[c0 + i] = (float)sgx;
+    }
+  }
+  team_sum<TEAM>(s0, s1, red);
+  const double n = (double)s.positions * s.per_group;
+  Slope sl[VEC];
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) sl[e] = Slope(ga[e], mu, is, s0 / n, s1 / n);
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    if (t + TEAM * j < count) {
+      float o[VEC];
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        o[e] = sl[e].dx(d[j][e], v[j][e]);
+      }
+      store_vec<VEC>(dx + from + j * step, o);
+      if (dskip) store_vec<VEC>(dskip + from + j * step, d[j]);
+    }
+}
+
+// Parameters' gradients: sums over `rows` rows of 2 C values; 16 values and 64 threads for each per block.
+__global__ __launch_bounds__(1024) void gn_parameters_kernel(const double* sums, int rows, int C, float* dgamma, float* dbeta) {
+  __shared__ double red[16][16];
+  const int lane = threadIdx.x & 15, at = threadIdx.x >> 4, i = blockIdx.x * 16 + lane;
+  double s = 0.0;
+  if (i < 2 * C) {
+    for (int r0 = at; r0 < rows; r0 += 64 * 8) {               // eight loads in flight
+      double v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = r0 + 64 * k < rows ? sums[(size_t)(r0 + 64 * k) * 2 * C + i] : 0.0;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s += v[k];
+    }
+  }
+  s += __shfl_xor(s, 16, 64);
+  s += __shfl_xor(s, 32, 64);
+  if ((threadIdx.x & 63) < 16) red[threadIdx.x >> 6][lane] = s;
+  __syncthreads();
+  if (threadIdx.x < 16 && i < 2 * C) {
+    s = 0.0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) s += red[w][lane];
+    if (i & 1) dgamma[i >> 1] = (float)s;
+    else dbeta[i >> 1] = (float)s;
+  }
+}
+
+// ---- larger groups: sums, statistics and values in launches of their own -----------------------------
 // Sums of a block's positions per channel: part[sample][chunk][channel][2].  Forward: of x - x0 and its square, x0 = the first value of
 // the sample's group, which keeps the digits of a group whose mean is large beside its spread.  BWD: of the error behind the
 // activation and of its product with xhat.  A thread takes VEC neighbouring channels, LANES threads a strip of channels.
@@ -112,12 +390,11 @@ __global__ __launch_bounds__(256) void gn_partial_kernel(const float* x, const f
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
         if (BWD) {
-          const double xh = nm[e].xhat(v[e]);
-          double z = nm[e].z(xh);
+          double z = nm[e].z(v[e]);
           if (ACT != XBAR_ACT_NONE && skip) z += (double)k[e];
           const double g = (double)act_bwd<ACT>(z, d[e]);
           s0[e] += g;
-          s1[e] = __builtin_fma(g, xh, s1[e]);
+          s1[e] = __builtin_fma(g, (double)v[e], s1[e]);
         } else {
           const double u = (double)v[e] - (double)x0[e];
           s0[e] += u;
@@ -143,6 +420,13 @@ __global__ __launch_bounds__(256) void gn_partial_kernel(const float* x, const f
     t = 0.0;
 #pragma unroll
     for (int k = 0; k < SHARES; ++k) t += shares[k][value];
+    if (BWD && value >= CT) {
+      double g = 0.0;
+#pragma unroll
+      for (int k = 0; k < SHARES; ++k) g += shares[k][value - CT];
+      const int item = b * s.groups + cv / s.per_group;
+      t = xhat_sum(g, t, mean[item], invstd[item]);
+    }
     part[((size_t)blockIdx.x * C + cv) * 2 + value / CT] = t;
   }
 }
@@ -183,35 +467,15 @@ __global__ __launch_bounds__(256) void gn_final_fwd_kernel(const double* part, S
   if (item < s.batch * s.groups) group_of_wave<false>(part, s, item, x, nullptr, eps, mean, invstd, nullptr);
 }
 
-// The first waves take a sample's group each, the others a channel: its parameters' gradients over the batch.
-__global__ __launch_bounds__(256) void gn_final_bwd_kernel(const double* part, Shape s, const float* gamma, double* coef, float* dgamma,
-                                                           float* dbeta) {
-  int item = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (item < s.batch * s.groups) {
-    group_of_wave<true>(part, s, item, nullptr, gamma, 0.0f, nullptr, nullptr, coef);
-    return;
-  }
-  item -= s.batch * s.groups;
-  if (item >= s.channels) return;
-  const int lane = threadIdx.x & 63, all = s.batch * s.chunks;
-  double s0 = 0.0, s1 = 0.0;
-  for (int i = lane; i < all; i += 64) {
-    s0 += part[((size_t)i * s.channels + item) * 2];
-    s1 += part[((size_t)i * s.channels + item) * 2 + 1];
-  }
-#pragma unroll
-  for (int d = 32; d; d >>= 1) {
-    s0 += __shfl_xor(s0, d, 64);
-    s1 += __shfl_xor(s1, d, 64);
-  }
-  if (lane == 0) {
-    dbeta[item] = (float)s0;
-    dgamma[item] = (float)s1;
-  }
+__global__ __launch_bounds__(256) void gn_final_bwd_kernel(const double* part, Shape s, const float* gamma, double* coef) {
+  const int item = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (item < s.batch * s.groups) group_of_wave<true>(part, s, item, nullptr, gamma, 0.0f, nullptr, nullptr, coef);
 }
 
-// y, or dx and dskip; blocks and threads as in gn_partial_kernel.
-template <bool BWD, int ACT, int VEC, int LANES>
+// y, or dx and dskip; blocks and threads as in gn_partial_kernel.  PAST: outputs of more than half of the last-level cache, which the next
+// reader would not find there, leave it to x (64 x 56 x 56 x 256 with a ReLU behind it 201 -> 187 us, alone 130 -> 112; 32 x 112 x 112 x 64, half as
+// much, 95 -> 100: there the ordinary way).
+template <bool BWD, int ACT, int VEC, int LANES, bool PAST>
 __global__ __launch_bounds__(256) void gn_apply_kernel(const float* x, const float* dy, const float* gamma, const float* beta,
                                                        const float* skip, const float* mean, const float* invstd, const double* coef,
                                                        float* out, float* dskip, Shape s) {
@@ -224,13 +488,12 @@ __global__ __launch_bounds__(256) void gn_apply_kernel(const float* x, const flo
   const int r0 = chunk * s.rows, r1 = min(r0 + s.rows, s.positions);
   Norm nm[VEC];
   load_norm<VEC>(nm, s, b, c, gamma, beta, mean, invstd);
-  double m0[VEC], m1[VEC];
+  Slope sl[VEC];
   if (BWD)
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
       const size_t g = (size_t)b * s.groups + (c + e) / s.per_group;
-      m0[e] = coef[g * 2];
-      m1[e] = coef[g * 2 + 1];
+      sl[e] = Slope(gamma[c + e], mean[g], invstd[g], coef[g * 2], coef[g * 2 + 1]);
     }
 #pragma unroll 4
   for (int r = r0 + grp; r < r1; r += G) {
@@ -241,18 +504,17 @@ __global__ __launch_bounds__(256) void gn_apply_kernel(const float* x, const flo
     if ((!BWD || ACT != XBAR_ACT_NONE) && skip) load_vec<VEC>(skip + at, k);
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
-      const double xh = nm[e].xhat(v[e]);
-      double z = nm[e].z(xh);
+      double z = nm[e].z(v[e]);
       if ((!BWD || ACT != XBAR_ACT_NONE) && skip) z += (double)k[e];
       if (BWD) {
         q[e] = act_bwd<ACT>(z, d[e]);
-        o[e] = (float)(nm[e].invstd * (nm[e].gamma * (double)q[e] - m0[e] - xh * m1[e]));
+        o[e] = sl[e].dx(q[e], v[e]);
       } else {
         o[e] = act_of<ACT>(z);
       }
     }
-    store_vec<VEC>(out + at, o);
-    if (BWD && dskip) store_vec<VEC>(dskip + at, q);
+    store_vec<VEC, PAST>(out + at, o);
+    if (BWD && dskip) store_vec<VEC, PAST>(dskip + at, q);
   }
 }
 
@@ -261,6 +523,7 @@ struct Plan {
   Shape s;
   int vec, lanes;
   dim3 grid;
+  int held_vec, elements;      // of a group held in registers: floats and number of its vectors
   Plan(int batch, int positions, int channels, int groups) {
     vec = channels % 4 == 0 ? 4 : 1;
     const int strip = channels <= 32 ? 16 : 64, strips = (channels + strip - 1) / strip;
@@ -270,6 +533,26 @@ struct Plan {
     const int chunks = (positions + rows - 1) / rows;
     s = Shape{batch, positions, channels, groups, channels / groups, rows, chunks};
     grid = dim3((unsigned)(batch * chunks), (unsigned)strips);
+    held_vec = s.per_group % 4 == 0 ? 4 : s.per_group % 2 == 0 ? 2 : 1;
+    elements = (int)std::min<long long>(1 << 30, (long long)positions * (s.per_group / held_vec));
+  }
+  bool past() const { return (double)s.batch * s.positions * s.channels * sizeof(float) > 134217728.0; }
+  // Threads that hold a group (0: too large, three launches instead).  Few threads where a few vectors each are enough, so that small groups
+  // share a block; 512 with eight vectors each at most: with 16 a block fills a compute unit and nothing hides its loads (64 x 56 x 56 x 256 in
+  // 32 groups, forward: 219 us, 200 with 1024 threads, against 167 in three launches).  us, held / three launches: forward 13 x 255 x 90 in 9
+  // groups 15.1 / 19.9, 1 x 64 x 64 14.9 / 19.0; backward 128 x 1024 x 16 in 4 groups 18.5 / 24, 64 x 784 x 512 in 32 92 / 107.
+  int team(bool backward) const {
+    const int q = s.per_group / held_vec, most = 512 * 8;
+    if (elements > most) return 0;
+    const int t = elements <= 32 ? 16 : elements <= 256 ? 64 : elements <= 1024 ? 256 : 512;
+    if (!backward) return t;
+    if (q & (q - 1)) return 0;                               // a thread's elements have to lie in the same channels
+    return t >= q ? t : q <= 64 ? 64 : q <= 256 ? 256 : q <= 512 ? 512 : 0;
+  }
+  dim3 held_grid(int team) const {
+    const int teams = team_block(team) / team;
+    const long long blocks = ((long long)s.batch * s.groups + teams - 1) / teams;
+    return dim3((unsigned)((blocks + kXcds - 1) / kXcds * kXcds));
   }
   size_t sums() const { return (size_t)s.batch * s.chunks * s.channels * 2; }
   size_t bytes() const { return align256(sums() * sizeof(double)) + align256((size_t)s.batch * s.groups * 2 * sizeof(double)); }
@@ -308,6 +591,35 @@ struct Bwd {
   float *dx, *dskip;
 };
 
+template <int ACT, int VEC>
+struct Held {
+  static int fwd(const Plan& p, const Fwd& a, float eps, hipStream_t st) {
+    const int team = p.team(false);
+    auto k = team == 16 ? gn_held_fwd_kernel<ACT, VEC, 16, 2> : team == 64 ? gn_held_fwd_kernel<ACT, VEC, 64, 4>
+             : team == 256 ? gn_held_fwd_kernel<ACT, VEC, 256, 4> : gn_held_fwd_kernel<ACT, VEC, 512, 8>;
+    hipLaunchKernelGGL(k, p.held_grid(team), dim3(team_block(team)), 0, st, a.x, a.gamma, a.beta, a.skip, a.y, a.mean, a.invstd, p.s, eps);
+    return launched();
+  }
+  static int bwd(const Plan& p, const Bwd& a, double* sums, float* dgamma, float* dbeta, hipStream_t st) {
+    const int team = p.team(true);
+    auto k = team == 16 ? gn_held_bwd_kernel<ACT, VEC, 16, 2> : team == 64 ? gn_held_bwd_kernel<ACT, VEC, 64, 4>
+             : team == 256 ? gn_held_bwd_kernel<ACT, VEC, 256, 4> : gn_held_bwd_kernel<ACT, VEC, 512, 8>;
+    hipLaunchKernelGGL(k, p.held_grid(team), dim3(team_block(team)), 0, st, a.x, a.dy, a.gamma, a.beta, a.skip, a.mean, a.invstd, a.dx, a.dskip,
+                       sums, dgamma, dbeta, p.s);
+    return launched();
+  }
+};
+template <class F>
+int with_held(int act, int vec, F f) {
+  auto with_act = [&](auto a) {
+    constexpr int ACT = decltype(a)::value;
+    return vec == 4 ? f(Held<ACT, 4>()) : vec == 2 ? f(Held<ACT, 2>()) : f(Held<ACT, 1>());
+  };
+  if (act == XBAR_ACT_RELU) return with_act(std::integral_constant<int, XBAR_ACT_RELU>());
+  if (act == XBAR_ACT_SILU) return with_act(std::integral_constant<int, XBAR_ACT_SILU>());
+  return with_act(std::integral_constant<int, XBAR_ACT_NONE>());
+}
+
 template <int ACT, int VEC, int LANES>
 struct PartialFwd {
   static void go(const Plan* p, const Fwd* a, double* part, hipStream_t st) {
@@ -318,8 +630,8 @@ struct PartialFwd {
 template <int ACT, int VEC, int LANES>
 struct ApplyFwd {
   static void go(const Plan* p, const Fwd* a, hipStream_t st) {
-    hipLaunchKernelGGL((gn_apply_kernel<false, ACT, VEC, LANES>), p->grid, dim3(256), 0, st, a->x, (const float*)nullptr, a->gamma, a->beta,
-                       a->skip, a->mean, a->invstd, (const double*)nullptr, a->y, (float*)nullptr, p->s);
+    auto k = VEC == 4 && p->past() ? gn_apply_kernel<false, ACT, VEC, LANES, VEC == 4> : gn_apply_kernel<false, ACT, VEC, LANES, false>;
+    hipLaunchKernelGGL(k, p->grid, dim3(256), 0, st, a->x, (const float*)nullptr, a->gamma, a->beta, a->skip, a->mean, a->invstd, (const double*)nullptr, a->y, (float*)nullptr, p->s);
   }
 };
 template <int ACT, int VEC, int LANES>
@@ -332,8 +644,8 @@ struct PartialBwd {
 template <int ACT, int VEC, int LANES>
 struct ApplyBwd {
   static void go(const Plan* p, const Bwd* a, const double* coef, hipStream_t st) {
-    hipLaunchKernelGGL((gn_apply_kernel<true, ACT, VEC, LANES>), p->grid, dim3(256), 0, st, a->x, a->dy, a->gamma, a->beta, a->skip, a->mean,
-                       a->invstd, coef, a->dx, a->dskip, p->s);
+    auto k = VEC == 4 && p->past() ? gn_apply_kernel<true, ACT, VEC, LANES, VEC == 4> : gn_apply_kernel<true, ACT, VEC, LANES, false>;
+    hipLaunchKernelGGL(k, p->grid, dim3(256), 0, st, a->x, a->dy, a->gamma, a->beta, a->skip, a->mean, a->invstd, coef, a->dx, a->dskip, p->s);
   }
 };
 
@@ -359,6 +671,7 @@ int xbar_gn_fwd(const float* x, const float* gamma, const float* beta, const flo
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   double* part = reinterpret_cast<double*>(ws);
   const Fwd a{x, gamma, beta, skip, y, mean, invstd};
+  if (p.team(false)) return with_held(act, p.held_vec, [&](auto k) { return k.fwd(p, a, eps, st); });
   dispatch<PartialFwd>(XBAR_ACT_NONE, p.vec, p.lanes, &p, &a, part, st);
   if (launched()) return XBAR_EHIP;
   hipLaunchKernelGGL(gn_final_fwd_kernel, dim3((unsigned)((batch * groups + 3) / 4)), dim3(256), 0, st, part, p.s, x, eps, mean, invstd);
@@ -385,10 +698,18 @@ int xbar_gn_bwd(const float* x, const float* dy, const float* gamma, const float
   double* part = reinterpret_cast<double*>(ws);
   double* coef = reinterpret_cast<double*>(reinterpret_cast<char*>(ws) + align256(p.sums() * sizeof(double)));
   const Bwd a{x, dy, gamma, beta, skip, mean, invstd, dx, dskip};
+  const dim3 parameters((unsigned)((2 * channels + 15) / 16));
+  if (p.team(true)) {
+    const int rc = with_held(act, p.held_vec, [&](auto k) { return k.bwd(p, a, part, dgamma, dbeta, st); });
+    if (rc || batch == 1) return rc;
+    hipLaunchKernelGGL(gn_parameters_kernel, parameters, dim3(1024), 0, st, part, batch, channels, dgamma, dbeta);
+    return launched();
+  }
   dispatch<PartialBwd>(act, p.vec, p.lanes, &p, &a, part, st);
   if (launched()) return XBAR_EHIP;
-  hipLaunchKernelGGL(gn_final_bwd_kernel, dim3((unsigned)((batch * groups + channels + 3) / 4)), dim3(256), 0, st, part, p.s, gamma, coef, dgamma,
-                     dbeta);
+  hipLaunchKernelGGL(gn_final_bwd_kernel, dim3((unsigned)((batch * groups + 3) / 4)), dim3(256), 0, st, part, p.s, gamma, coef);
+  if (launched()) return XBAR_EHIP;
+  hipLaunchKernelGGL(gn_parameters_kernel, parameters, dim3(1024), 0, st, part, batch * p.s.chunks, channels, dgamma, dbeta);
   if (launched()) return XBAR_EHIP;
   dispatch<ApplyBwd>(act, p.vec, p.lanes, &p, &a, coef, st);
   return launched();

@@ -629,8 +629,9 @@ def absmax(x, ws=None):
 
 def _here(*tensors):
     """The library launches on the current device: its tensors have to lie there."""
-    device = torch.cuda.current_device()
-    assert all(t is None or t.get_device() == device for t in tensors), "a tensor is not on the current device"
+    device = torch.cuda.current_device() if _current_device is None else _current_device()
+    for t in tensors:
+        assert t is None or t.get_device() == device, "a tensor is not on the current device"
 
 
 def _gn_ws(batch, positions, channels, groups, ws, device):
