@@ -38,6 +38,8 @@ class CrossbarLayer:
         self.x_scale = self.g_scale = 1.0
         self.planes = torch.empty(xb.planes_bytes(self.cfg, K, N), dtype=torch.uint8, device=device)
         self.x = None
+        self.programmed = False            # the planes hold W as it is (only a frozen network asks)
+        self.adapters = None               # low-rank adapters beside the projection (Network.add_adapters)
         self.profile = None                # stored wire distortion (with the profile flag), refreshed by forward()
         self.pair = None                   # (Gp, Gn) once the network updates the two devices of a weight separately
         self.seen_x = self.seen_g = None   # set while the ranges are being calibrated
@@ -46,6 +48,19 @@ class CrossbarLayer:
         ops = self.net.ops
         if self.net.calibrating and self.net.adc_quantile is None:
             self.seen_x = self.x_scale = ops.absmax(x) or 1.0
+        if not (self.net.frozen and self.programmed):
+            self._program(step, ws)
+        self.programmed = self.net.frozen
+        self.x = x
+        if self.net.adc_quantile is not None:
+            self.cfg.adc_fs_fwd = self._measured_range(xb.OP_FWD, x, self.x_scale, self.cfg.xbar_rows, ws)
+        if self.geom is None:
+            y = ops.fwd(self.cfg, self.planes, x, self.N, self.w_max, self.x_scale, ws=ws)
+            return y if self._plan() is None else self.adapters.forward(self._plan(), y, x)
+        return ops.conv_fwd(self.cfg, self.planes, x, self.geom, self.N, self.w_max, self.x_scale, ws=ws)
+
+    def _program(self, step, ws):
+        ops = self.net.ops
         if self.cfg.flags & xb.NI_WIRE_PROFILE:
             # the circuit-level model every `fcm_every` steps, its stored distortion profile in between (Sec. IV-D)
             if self.profile is None or step % self.net.fcm_every == 0:
@@ -53,17 +68,16 @@ class CrossbarLayer:
             ops.tile(self.cfg, self.W, self.w_max, step, self.profile, planes=self.planes)
         else:
             ops.tile(self.cfg, self.W, self.w_max, step, planes=self.planes)
-        self.x = x
-        if self.net.adc_quantile is not None:
-            self.cfg.adc_fs_fwd = self._measured_range(xb.OP_FWD, x, self.x_scale, self.cfg.xbar_rows, ws)
-        if self.geom is None:
-            return ops.fwd(self.cfg, self.planes, x, self.N, self.w_max, self.x_scale, ws=ws)
-        return ops.conv_fwd(self.cfg, self.planes, x, self.geom, self.N, self.w_max, self.x_scale, ws=ws)
+
+    def _plan(self):
+        """The batch's adapter plan, where this layer has adapters."""
+        return self.net.requests if self.adapters is not None else None
 
     def backward(self, dy, step, lr, ws, need_dx=True):
-        """Error to the layer input through the same conductances, then the in-place write of W (skipped
-        while the ranges are being calibrated)."""
+        """Error to the layer input through the same conductances (and the adapters beside them), then the in-place write of W
+        (skipped while the ranges are being calibrated and in a frozen network)."""
         ops = self.net.ops
+        writes = not self.net.calibrating and not self.net.frozen
         if self.net.calibrating and self.net.adc_quantile is None:
             self.seen_g = self.g_scale = ops.absmax(dy) or 1.0
         if self.net.adc_quantile is not None:
@@ -73,24 +87,26 @@ class CrossbarLayer:
         if self.geom is None:
             if need_dx:
                 dx = ops.bwd(self.cfg, self.planes, dy, self.K, self.w_max, self.g_scale, ws=ws)
-            if not self.net.calibrating and pulse is None and self.net.pair_devices:
+            if writes and pulse is None and self.net.pair_devices:
                 ops.update_pair(self.cfg, *self._pair(), self.W, self.x, dy, self.w_max, 1.0 / self.w_max, lr, step, ws=ws)
-            elif not self.net.calibrating and pulse is None:
+            elif writes and pulse is None:
                 ops.update(self.cfg, self.W, self.x, dy, self.w_max, 1.0 / self.w_max, lr, step, ws=ws)
-            elif not self.net.calibrating:
+            elif writes:
                 # inputs fire in proportion to their size over the calibrated range; the error range then follows
                 # from the learning rate: mean change = lr x dy / w_max  <=>  x_range d_range = bl dw_min w_max / lr
                 bl, dw_min, d_range = self._pulse_ranges(pulse, lr)
                 ops.update_pulsed(self.cfg, self.W, self.x, dy, self.w_max, self.x_scale, d_range, bl, dw_min, step, ws=ws)
+            if self._plan() is not None:
+                dx = self.adapters.backward(self._plan(), dx, dy, self.x, lr)
         else:
             if need_dx:
                 dx = ops.conv_bwd(self.cfg, self.planes, dy, self.geom, self.N, self.w_max, self.g_scale, ws=ws)
-            if not self.net.calibrating and pulse is None and self.net.pair_devices:
+            if writes and pulse is None and self.net.pair_devices:
                 ops.conv_update_pair(self.cfg, *self._pair(), self.W, self.x, dy, self.geom, self.w_max, 1.0 / self.w_max, lr,
                                      step, ws=ws)
-            elif not self.net.calibrating and pulse is None:
+            elif writes and pulse is None:
                 ops.conv_update(self.cfg, self.W, self.x, dy, self.geom, self.w_max, 1.0 / self.w_max, lr, step, ws=ws)
-            elif not self.net.calibrating:     # every output position is one sample of the pulse scheme
+            elif writes:     # every output position is one sample of the pulse scheme
                 bl, dw_min, d_range = self._pulse_ranges(pulse, lr)
                 ops.conv_update_pulsed(self.cfg, self.W, self.x, dy, self.geom, self.w_max, self.x_scale, d_range, bl,
                                        dw_min, step, ws=ws)
@@ -134,6 +150,33 @@ class CrossbarLayer:
         return max(fcm, *(xb.conv_workspace_bytes(self.cfg, op, self.geom, self.N) for op in (xb.OP_FWD, xb.OP_BWD, xb.OP_UPDATE, xb.OP_UPDATE_PULSED)))
 
 
+class Adapters:
+    """Low-rank adapters of several tasks beside one weight layer: the devices stay as they are programmed, every row of a batch gets the
+    digital correction scale A^T B of its request's adapter."""
+
+    def __init__(self, net, K, N, count, rank, scale, gen, device):
+        self.net = net
+        self.A = torch.randn((count, rank, K), generator=gen, device=device, dtype=torch.float32) / math.sqrt(K)
+        self.B = torch.zeros((count, rank, N), dtype=torch.float32, device=device)       # no correction before the first step
+        self.scale = torch.full((count,), float(scale), dtype=torch.float32, device=device)
+        self.T = None
+
+    def compact(self):
+        """bfloat16 adapters: half the memory for serving; they are not trained any more."""
+        self.A, self.B = self.A.to(torch.bfloat16), self.B.to(torch.bfloat16)
+
+    def forward(self, plan, y, x):
+        _, self.T = self.net.ops.adapter_fwd(plan, y, x, self.A, self.B, self.scale, out=y)
+        return y
+
+    def backward(self, plan, dx, dy, x, lr):
+        """dx (or None) with the adapters' share of the error added in place; then the parameters' step."""
+        _, dA, dB = self.net.ops.adapter_bwd(plan, dx, dy, x, self.T, self.A, self.B, self.scale, out=dx)
+        if self.A.dtype is torch.float32:
+            self.net.step_digital(((self.A, dA), (self.B, dB)), lr)
+        return dx
+
+
 class BatchNorm:
     def __init__(self, net, channels, device):
         self.net = net
@@ -168,12 +211,55 @@ class BatchNorm:
         x, mean, invstd = self.saved
         ops = self.net.ops
         if self.net.joins_passes():
-            return ops.bn_bwd_sgd(x, dy, self.gamma, self.beta, mean, invstd, relu, None if self.net.calibrating else lr, ws=ws)[0]
+            clips = self.net.max_grad_norm is not None
+            dx, dgamma, dbeta = ops.bn_bwd_sgd(x, dy, self.gamma, self.beta, mean, invstd, relu,
+                                               None if self.net.calibrating or clips else lr, ws=ws)
+            if clips:
+                self.net.step_digital(((self.gamma, dgamma), (self.beta, dbeta)), lr)
+            return dx
         dx, dgamma, dbeta = ops.bn_bwd(x, dy, self.gamma, mean, invstd, ws=ws)
-        if not self.net.calibrating:
-            ops.sgd(self.gamma, dgamma, lr)
-            ops.sgd(self.beta, dbeta, lr)
+        self.net.step_digital(((self.gamma, dgamma), (self.beta, dbeta)), lr)
         return dx
+
+
+class GroupNorm:
+    """Normalisation per sample and group of channels: what BatchNorm is to a batch, for small batches and single requests."""
+
+    def __init__(self, net, channels, device, groups):
+        self.net, self.groups = net, groups
+        self.gamma = torch.ones(channels, dtype=torch.float32, device=device)
+        self.beta = torch.zeros(channels, dtype=torch.float32, device=device)
+        self.saved = None
+
+    def forward(self, x, ws, act=xb.ACT_NONE, skip=None):
+        y, mean, invstd = self.net.ops.gn_fwd(x, self.gamma, self.beta, self.groups, 1e-5, act, skip, ws=ws)
+        self.saved = (x, mean, invstd)
+        return y
+
+    def forward_relu(self, x, ws, skip=None):
+        """relu(normalised x + skip); skip: a tensor or a function that gives one."""
+        return self.forward(x, ws, xb.ACT_RELU, skip() if callable(skip) else skip)
+
+    def backward_relu(self, y, dy, lr, ws):
+        """Error through the ReLU whose output y was (forward_relu without a skip) and the normalisation."""
+        return self.backward(dy, lr, ws, xb.ACT_RELU)
+
+    def backward(self, dy, lr, ws, act=xb.ACT_NONE):
+        x, mean, invstd = self.saved
+        dx, dgamma, dbeta = self.net.ops.gn_bwd(x, dy, self.gamma, self.beta, mean, invstd, act, ws=ws)
+        self.net.step_digital(((self.gamma, dgamma), (self.beta, dbeta)), lr)
+        return dx
+
+
+def make_norm(net, kind, groups, channels, positions, device):
+    """The normalisation behind a layer: "batch", or "group" with at most `groups` groups (what divides the channels)."""
+    if kind == "group":
+        groups = math.gcd(groups, channels)
+        net.norm_bytes = max(net.norm_bytes, xb.lib().xbar_gn_workspace_bytes(net.batch, positions, channels, groups))
+        return GroupNorm(net, channels, device, groups)
+    if kind != "batch":
+        raise ValueError("unknown normalisation %r" % (kind,))
+    return BatchNorm(net, channels, device)
 
 
 class Network:
@@ -186,6 +272,12 @@ class Network:
     fcm_every = 1         # with the stored-profile wire model: steps between two runs of the circuit-level model
     adc_quantile = None   # set while the converter ranges are being measured
     pulse = None     # dict(bl=slots per train, dw_min=state change per pulse): pulse-level updates of the crossbar layers
+    frozen = False   # the crossbars keep their conductances: programmed at the first forward pass, read ever after; digital parameters learn
+    max_grad_norm = None   # set: the digital parameters (normalisations, adapters) step together, their gradients clipped to this global norm
+    grad_norm = None   # the norm that their gradients had in the last such step (device tensor)
+    _pending = ()     # (parameter, gradient) pairs of the step so far
+    requests = None   # plan of the batch's adapters (set_requests)
+    norm_bytes = 0    # workspace of the widest group normalisation
     pair_devices = False   # aggregate updates keep the positive and the negative device of a weight as states of their own
 
     def joins_passes(self):
@@ -200,12 +292,42 @@ class Network:
             return ops.add(a, b)
         return ops.add_relu_bwd(out, a, b) if self.joins_passes() else ops.relu_bwd(out, ops.add(a, b))
 
+    def step_digital(self, pairs, lr):
+        """SGD step of digital parameters from their gradients: at once, or -- where they are clipped together -- with all others at the
+        end of the step.  Nothing while the ranges are being calibrated."""
+        if self.calibrating:
+            return
+        if self.max_grad_norm is not None:
+            self._pending = (*self._pending, *pairs)
+            return
+        for p, g in pairs:
+            self.ops.sgd(p, g, lr)
+
+    def _finish_step(self, lr):
+        pending, self._pending = self._pending, ()
+        if pending:
+            self.grad_norm = self.ops.clip_sgd([p for p, _ in pending], [g for _, g in pending], lr, self.max_grad_norm)
+
+    def add_adapters(self, count, rank, scale=1.0, seed=0):
+        """`count` low-rank adapters beside every fully connected layer; which row of a batch uses which: set_requests."""
+        for layer in self.layers:
+            if layer.geom is None:
+                gen = torch.Generator(device=layer.W.device)
+                gen.manual_seed(seed + layer.index)
+                layer.adapters = Adapters(self, layer.K, layer.N, count, rank, scale, gen, layer.W.device)
+        self.adapter_count = count
+
+    def set_requests(self, rows):
+        """The adapter of every row of the next batches (int32 tensor; none: a negative number), or None: no adapters."""
+        self.requests = None if rows is None else self.ops.adapter_plan(rows, self.adapter_count)
+
     def train_step(self, x, labels, lr):
         """One SGD step on a batch: returns the per-sample losses (device tensor)."""
-        step = self.step_no
+        step, self._pending = self.step_no, ()
         logits = self.forward(x, step)
         loss, dlogits = self.ops.softmax_xent(logits, labels, 1.0 / x.shape[0])
         self.backward(dlogits, step, lr)
+        self._finish_step(lr)
         self.step_no += 1
         return loss
 
@@ -252,6 +374,7 @@ class Network:
         logits = self.forward(self._graph_x, 0)
         loss, dlogits = self.ops.softmax_xent(logits, self._graph_labels, 1.0 / self._graph_x.shape[0])
         self.backward(dlogits, 0, lr)
+        self._finish_step(lr)
         self.ops.step_advance(self._graph_counter)
         return loss
 
@@ -287,27 +410,29 @@ class Network:
 
 
 class ResNetCifar(Network):
-    def __init__(self, cfg_kwargs, batch, n_blocks=3, image=32, classes=10, widths=(16, 32, 64), seed=0, device="cuda"):
+    def __init__(self, cfg_kwargs, batch, n_blocks=3, image=32, classes=10, widths=(16, 32, 64), seed=0, device="cuda", norm="batch", groups=8):
+        """norm: "batch", or "group" in `groups` groups of channels."""
         gen = torch.Generator(device=device)
         gen.manual_seed(seed)
         self.batch, self.image, self.classes = batch, image, classes
         conv = lambda hw, cin, cout, stride, signed: CrossbarLayer(
             self, cfg_kwargs, 9 * cin, cout, xb.conv_geom(batch, hw, hw, cin, 3, 3, stride, 1), signed, gen, device)
-        self.stem, self.stem_bn = conv(image, 3, widths[0], 1, True), BatchNorm(self, widths[0], device)
+        normed = lambda hw, width: make_norm(self, norm, groups, width, hw * hw, device)
+        self.stem, self.stem_bn = conv(image, 3, widths[0], 1, True), normed(image, widths[0])
         self.blocks = []
         cin, hw = widths[0], image
         for stage, width in enumerate(widths):
             for b in range(n_blocks):
                 stride = 2 if (b == 0 and stage > 0) else 1
                 hw_out = (hw + stride - 1) // stride
-                self.blocks.append(dict(a=conv(hw, cin, width, stride, False), bn_a=BatchNorm(self, width, device),
-                                        b=conv(hw_out, width, width, 1, False), bn_b=BatchNorm(self, width, device),
+                self.blocks.append(dict(a=conv(hw, cin, width, stride, False), bn_a=normed(hw_out, width),
+                                        b=conv(hw_out, width, width, 1, False), bn_b=normed(hw_out, width),
                                         stride=stride, cin=cin, width=width))
                 cin, hw = width, hw_out
         self.fc = CrossbarLayer(self, cfg_kwargs, cin, classes, None, False, gen, device)
         self.layers = [self.stem] + [blk[k] for blk in self.blocks for k in ("a", "b")] + [self.fc]
         nbytes = max(max(L.workspace_bytes(batch) for L in self.layers),
-                     xb.lib().xbar_bn_workspace_bytes(batch * image * image, max(widths)), 4096)
+                     xb.lib().xbar_bn_workspace_bytes(batch * image * image, max(widths)), self.norm_bytes, 4096)
         self.ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
         self.step_no = 0
 

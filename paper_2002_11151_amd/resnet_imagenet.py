@@ -8,12 +8,13 @@ its CIFAR-size sibling this module only sequences calls of the C-ABI binding.
 import torch
 
 from . import xbar as xb
-from .resnet_cifar import BatchNorm, CrossbarLayer, Network
+from .resnet_cifar import CrossbarLayer, Network, make_norm
 
 
 class ResNetBottleneck(Network):
     def __init__(self, cfg_kwargs, batch, image=224, classes=1000, blocks=(3, 4, 6, 3), widths=(64, 128, 256, 512),
-                 stem=64, seed=0, device="cuda"):
+                 stem=64, seed=0, device="cuda", norm="batch", groups=32):
+        """norm: "batch", or "group" in `groups` groups of channels."""
         gen = torch.Generator(device=device)
         gen.manual_seed(seed)
         self.batch = batch
@@ -22,8 +23,9 @@ class ResNetBottleneck(Network):
             return CrossbarLayer(self, cfg_kwargs, k * k * cin, cout, xb.conv_geom(batch, hw, hw, cin, k, k, stride, pad),
                                  signed, gen, device)
 
-        self.stem, self.stem_bn = conv(image, 3, stem, 7, 2, 3, True), BatchNorm(self, stem, device)
+        normed = lambda hw, width: make_norm(self, norm, groups, width, hw * hw, device)
         hw = (image + 6 - 7) // 2 + 1
+        self.stem, self.stem_bn = conv(image, 3, stem, 7, 2, 3, True), normed(hw, stem)
         self.pool_geom = xb.conv_geom(batch, hw, hw, stem, 3, 3, 2, 1)
         hw = self.pool_geom.out_h
         self.blocks = []
@@ -32,18 +34,18 @@ class ResNetBottleneck(Network):
             for b in range(n):
                 stride = 2 if (b == 0 and stage > 0) else 1
                 hw_out = (hw + 2 - 3) // stride + 1
-                blk = dict(a=conv(hw, cin, width, 1, 1, 0), bn_a=BatchNorm(self, width, device),
-                           b=conv(hw, width, width, 3, stride, 1), bn_b=BatchNorm(self, width, device),
-                           c=conv(hw_out, width, 4 * width, 1, 1, 0), bn_c=BatchNorm(self, 4 * width, device))
+                blk = dict(a=conv(hw, cin, width, 1, 1, 0), bn_a=normed(hw, width),
+                           b=conv(hw, width, width, 3, stride, 1), bn_b=normed(hw_out, width),
+                           c=conv(hw_out, width, 4 * width, 1, 1, 0), bn_c=normed(hw_out, 4 * width))
                 if b == 0:                              # projection shortcut (changes width and, later, size)
-                    blk["down"], blk["bn_down"] = conv(hw, cin, 4 * width, 1, stride, 0), BatchNorm(self, 4 * width, device)
+                    blk["down"], blk["bn_down"] = conv(hw, cin, 4 * width, 1, stride, 0), normed(hw_out, 4 * width)
                 self.blocks.append(blk)
                 cin, hw = 4 * width, hw_out
         self.fc = CrossbarLayer(self, cfg_kwargs, cin, classes, None, False, gen, device)
         self.layers = [self.stem] + [blk[k] for blk in self.blocks for k in ("a", "b", "c", "down") if k in blk] + [self.fc]
         rows = batch * ((image + 6 - 7) // 2 + 1) ** 2
         nbytes = max(max(L.workspace_bytes(batch) for L in self.layers),
-                     xb.lib().xbar_bn_workspace_bytes(rows, max(stem, 4 * max(widths))), 4096)
+                     xb.lib().xbar_bn_workspace_bytes(rows, max(stem, 4 * max(widths))), self.norm_bytes, 4096)
         self.ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
         self.step_no = 0
 

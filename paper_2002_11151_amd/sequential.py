@@ -5,12 +5,12 @@ the C-ABI binding.
 
 A network is a list of layer specs:
     ("conv", out_channels, kernel, stride, pad) | ("relu",) | ("sigmoid",) | ("maxpool", kernel, stride) |
-    ("flatten",) | ("fc", out_features)
+    ("groupnorm", groups, "none" | "relu" | "silu") | ("flatten",) | ("fc", out_features)
 """
 import torch
 
 from . import xbar as xb
-from .resnet_cifar import CrossbarLayer, Network
+from .resnet_cifar import CrossbarLayer, GroupNorm, Network
 
 
 def vgg16_spec(classes=1000):
@@ -61,6 +61,17 @@ class Sequential(Network):
                 geom = xb.conv_geom(batch, h, w, c, op[1], op[1], op[2], 0)
                 self.stack.append(("maxpool", geom))
                 shape = (geom.out_h, geom.out_w, c)
+            elif kind == "groupnorm":
+                act = ("none", "relu", "silu").index(op[2])
+                positions = 1
+                for d in shape[:-1]:
+                    positions *= d
+                nbytes = xb.lib().xbar_gn_workspace_bytes(batch, positions, shape[-1], op[1])
+                if nbytes == 0:
+                    raise ValueError("group normalisation of %d channels in %d groups" % (shape[-1], op[1]))
+                self.norm_bytes = max(self.norm_bytes, nbytes)
+                self.stack.append((kind, (GroupNorm(self, shape[-1], device, op[1]), act)))
+                signed = act != xb.ACT_RELU
             elif kind == "flatten":
                 n = 1
                 for d in shape:
@@ -69,7 +80,7 @@ class Sequential(Network):
                 shape = (n,)
             else:
                 raise ValueError("unknown layer spec %r" % (op,))
-        self.ws = torch.empty(max(max(L.workspace_bytes(batch) for L in self.layers), 4096), dtype=torch.uint8,
+        self.ws = torch.empty(max(max(L.workspace_bytes(batch) for L in self.layers), self.norm_bytes, 4096), dtype=torch.uint8,
                               device=device)
         self.saved = [None] * len(self.stack)
         self.step_no = 0
@@ -84,6 +95,8 @@ class Sequential(Network):
             elif kind == "sigmoid":
                 x = self.ops.sigmoid_fwd(x)
                 self.saved[i] = x
+            elif kind == "groupnorm":
+                x = arg[0].forward(x, self.ws, arg[1])
             elif kind == "maxpool":
                 x, self.saved[i] = self.ops.maxpool_fwd(x, arg)
             else:                                             # flatten: NHWC rows are already contiguous
@@ -101,6 +114,8 @@ class Sequential(Network):
                 d = self.ops.relu_bwd(self.saved[i], d)
             elif kind == "sigmoid":
                 d = self.ops.sigmoid_bwd(self.saved[i], d)
+            elif kind == "groupnorm":
+                d = arg[0].backward(d, lr, self.ws, arg[1])
             elif kind == "maxpool":
                 d = self.ops.maxpool_bwd(d, self.saved[i], arg)
             else:

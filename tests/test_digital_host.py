@@ -162,3 +162,160 @@ def test_binding_checks_lists_and_devices(xb):
         xb.gn_fwd(torch.zeros(2, 4), torch.ones(4), torch.zeros(4), 2)
     with pytest.raises((AssertionError, RuntimeError)):
         xb.adapter_plan(torch.zeros(4, dtype=torch.int32), 2)
+
+
+# ---- networks --------------------------------------------------------------------------------------
+def _stand_in(xb):
+    torch = pytest.importorskip("torch")
+    from test_network_host import StandIn
+
+    class Ops(StandIn):
+        """With the digital operators, from their definitions."""
+
+        def tile(self, cfg, W, w_max, step=0, profile=None, planes=None):
+            self.programmed = getattr(self, "programmed", {})
+            self.programmed[planes.data_ptr()] = W.clone()
+            return super().tile(cfg, W, w_max, step, profile, planes)
+
+        def fwd(self, cfg, planes, x, N, w_max, x_scale, ws=None):
+            self.W = self.programmed[planes.data_ptr()]
+            return super().fwd(cfg, planes, x, N, w_max, x_scale, ws)
+
+        def bwd(self, cfg, planes, dy, K, w_max, g_scale, ws=None):
+            self.W = self.programmed[planes.data_ptr()]
+            return super().bwd(cfg, planes, dy, K, w_max, g_scale, ws)
+
+        def adapter_plan(self, rows, n):
+            self._log("adapter_plan", n=n)
+            return rows
+
+        def adapter_fwd(self, plan, base, X, A, B, scale, out=None, ws=None):
+            self._log("adapter_fwd", in_place=out is base)
+            Y, T = digital.adapter_fwd(plan.numpy(), base.numpy(), X.numpy(), A.numpy(), B.numpy(), scale.numpy())
+            out.copy_(torch.from_numpy(Y))
+            return out, torch.from_numpy(T).float()
+
+        def adapter_bwd(self, plan, base, dY, X, T, A, B, scale, out=None, ws=None):
+            self._log("adapter_bwd", wants_dx=base is not None)
+            f = lambda t: t.numpy()
+            dX, dA, dB, _ = digital.adapter_bwd(f(plan), np.zeros(X.shape) if base is None else f(base), f(dY), f(X), f(T), f(A), f(B), f(scale))
+            if out is not None:
+                out.copy_(torch.from_numpy(dX))
+            return out, torch.from_numpy(dA).float(), torch.from_numpy(dB).float()
+
+        def gn_fwd(self, x, gamma, beta, groups, eps, act, skip=None, ws=None):
+            self._log("gn_fwd", groups=groups, act=act)
+            mean, invstd = digital.gn_stats(x.numpy(), groups, eps)
+            z = digital.gn_z(x.numpy(), gamma.numpy(), beta.numpy(), mean, invstd)[1]
+            return (torch.from_numpy(digital.act(z, ("none", "relu", "silu")[act])).float(), torch.from_numpy(mean).float(),
+                    torch.from_numpy(invstd).float())
+
+        def gn_bwd(self, x, dy, gamma, beta, mean, invstd, act, skip=None, ws=None):
+            self._log("gn_bwd", act=act)
+            got = digital.gn_bwd(*(t.numpy() for t in (x, dy, gamma, beta, mean, invstd)), ("none", "relu", "silu")[act])
+            return tuple(torch.from_numpy(t).float() for t in got[:3])
+
+        def sgd(self, p, g, lr):
+            self._log("sgd", size=p.numel())
+            p.sub_(lr * g)
+
+        def clip_sgd(self, params, grads, lr, max_norm):
+            norm = digital.grad_norm([g.numpy() for g in grads])
+            self._log("clip_sgd", tensors=len(params), max_norm=max_norm)
+            c = digital.clip_factor(norm, max_norm)
+            for p, g in zip(params, grads):
+                p.sub_(lr * c * g)
+            return torch.tensor([norm])
+    return Ops(xb)
+
+
+def _network(xb, spec, flags=0):
+    import workloads
+    from paper_2002_11151_amd import resnet_cifar, sequential
+    ops = _stand_in(xb)
+    resnet_cifar.Network.ops = ops
+    try:
+        net = sequential.Sequential(workloads.config_kwargs("mlp"), spec, batch=6, in_shape=(12,), signed_input=False, seed=1, device="cpu")
+    finally:
+        resnet_cifar.Network.ops = xb
+    net.ops = ops
+    return net, ops
+
+
+def _batch():
+    torch = pytest.importorskip("torch")
+    g = torch.Generator().manual_seed(0)
+    return torch.rand((6, 12), generator=g), (torch.arange(6) % 5).to(torch.int32)
+
+
+SPEC = [("flatten",), ("fc", 20), ("groupnorm", 4, "silu"), ("fc", 5)]
+
+
+def test_frozen_network_trains_its_digital_parameters(xb):
+    """The crossbars are programmed once and not written; adapters and normalisation step together, clipped."""
+    import torch
+    net, ops = _network(xb, SPEC)
+    x, labels = _batch()
+    net.calibrate(x, labels)
+    net.frozen, net.max_grad_norm = True, 0.25
+    net.add_adapters(2, 3, scale=2.0)
+    net.set_requests(torch.tensor([0, 1, -1, 1, 0, 0], dtype=torch.int32))
+    weights = [L.W.clone() for L in net.layers]
+    gamma = net.stack[2][1][0].gamma.clone()
+    ops.calls.clear()
+    for _ in range(2):
+        net.train_step(x, labels, 0.1)
+    names = [c[0] for c in ops.calls]
+    once = ["fwd", "adapter_fwd", "gn_fwd", "fwd", "adapter_fwd", "bwd", "adapter_bwd", "gn_bwd", "adapter_bwd", "clip_sgd"]
+    assert names == ["tile"] + once[:3] + ["tile"] + once[3:] + once
+    assert [c[1]["tensors"] for c in ops.calls if c[0] == "clip_sgd"] == [6, 6]
+    assert [c[1]["wants_dx"] for c in ops.calls if c[0] == "adapter_bwd"][:2] == [True, False]
+    assert all(torch.equal(L.W, w) for L, w in zip(net.layers, weights))
+    assert not torch.equal(net.stack[2][1][0].gamma, gamma) and all(L.adapters.B.any() for L in net.layers) and float(net.grad_norm) > 0
+    # unfrozen again, the devices are written and programmed anew
+    net.frozen = False
+    ops.calls.clear()
+    net.train_step(x, labels, 0.1)
+    assert [c[0] for c in ops.calls].count("tile") == 2 and [c[0] for c in ops.calls].count("update") == 2
+
+
+def test_digital_parameters_step_one_by_one_without_a_limit(xb):
+    import torch
+    net, ops = _network(xb, SPEC)
+    x, labels = _batch()
+    net.calibrate(x, labels)
+    assert not [c for c in ops.calls if c[0] in ("sgd", "clip_sgd", "update")]
+    net.add_adapters(2, 3)
+    net.set_requests(torch.zeros(6, dtype=torch.int32))
+    ops.calls.clear()
+    net.train_step(x, labels, 0.1)
+    assert [c[1]["size"] for c in ops.calls if c[0] == "sgd"] == [2 * 3 * 20, 2 * 3 * 5, 20, 20, 2 * 3 * 12, 2 * 3 * 20]
+    net.set_requests(None)
+    ops.calls.clear()
+    net.train_step(x, labels, 0.1)
+    assert not [c for c in ops.calls if c[0].startswith("adapter")]
+    # a step that an error cut short leaves nothing behind
+    net.max_grad_norm = 1.0
+    net._pending = ((x, x),)
+    ops.calls.clear()
+    net.train_step(x, labels, 0.1)
+    assert [c[1]["tensors"] for c in ops.calls if c[0] == "clip_sgd"] == [2]
+
+
+def test_normalisations_of_the_residual_networks(xb):
+    import workloads
+    from paper_2002_11151_amd import resnet_cifar, resnet_imagenet
+    ops = _stand_in(xb)
+    resnet_cifar.Network.ops = ops
+    try:
+        kw = workloads.config_kwargs("resnet20")
+        net = resnet_cifar.ResNetCifar(kw, batch=1, n_blocks=1, image=8, widths=(12, 16, 32), device="cpu", norm="group", groups=8)
+        assert [net.stem_bn.groups] + [b["bn_b"].groups for b in net.blocks] == [4, 4, 8, 8] and net.norm_bytes > 0
+        deep = resnet_imagenet.ResNetBottleneck(kw, batch=1, image=32, classes=10, blocks=(1, 1), widths=(16, 32), stem=16, device="cpu", norm="group")
+        assert deep.blocks[0]["bn_c"].groups == 32 and deep.blocks[1]["bn_down"].groups == 32
+        with pytest.raises(ValueError):
+            resnet_cifar.ResNetCifar(kw, batch=1, n_blocks=1, image=8, device="cpu", norm="layer")
+        with pytest.raises(ValueError):
+            _network(xb, [("flatten",), ("fc", 20), ("groupnorm", 3, "relu"), ("fc", 5)])
+    finally:
+        resnet_cifar.Network.ops = xb

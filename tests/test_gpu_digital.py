@@ -349,3 +349,120 @@ def test_another_stream_and_a_captured_graph(xb):
         torch.cuda.synchronize()
         for k in (0, 1):
             assert all(torch.equal(a, b) for a, b in zip(outs[k], want[k]))
+
+
+# ---- networks --------------------------------------------------------------------------------------
+class Recorder:
+    """The binding, keeping what the digital operators were given and gave."""
+    joins_passes = True
+
+    def __init__(self, xb):
+        self.xb, self.calls = xb, []
+
+    def __getattr__(self, name):
+        real = getattr(self.xb, name)
+        if name not in ("adapter_fwd", "adapter_bwd", "gn_fwd", "gn_bwd", "clip_sgd", "update", "fwd", "bwd"):
+            return real
+
+        def call(*args, **kw):
+            copy = lambda v: v.clone() if torch.is_tensor(v) else [copy(t) for t in v] if isinstance(v, list) else v
+            given = [copy(a) for a in args]
+            got = real(*args, **kw)
+            self.calls.append((name, given, copy(got) if torch.is_tensor(got) else tuple(copy(t) for t in got)))
+            return got
+        return call
+
+
+def perceptron(xb, seed=2):
+    import workloads
+    from paper_2002_11151_amd import sequential
+    spec = [("flatten",), ("fc", 60), ("groupnorm", 6, "silu"), ("fc", 10)]
+    net = sequential.Sequential(workloads.config_kwargs("mlp"), spec, batch=24, in_shape=(50,), signed_input=False, seed=seed)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    x = torch.rand((24, 50), generator=gen, device="cuda")
+    labels = (torch.arange(24, device="cuda") % 10).to(torch.int32)
+    net.calibrate(x, labels)
+    net.frozen, net.max_grad_norm = True, 0.05
+    net.add_adapters(3, 4)
+    for L in net.layers:
+        L.adapters.B.normal_(generator=gen).mul_(0.1)
+    net.set_requests(dev([0, 1, 2, -1] * 6, np.int32))
+    return net, x, labels
+
+
+def test_step_of_a_frozen_network(xb):
+    """One step of adapters and normalisation beside fixed crossbars, all operators together: the parameters move by the clipped gradients, which
+    are those of the definitions on what went through the crossbars."""
+    net, x, labels = perceptron(xb)
+    net.ops = Recorder(xb)
+    layers, norm = net.layers, net.stack[2][1][0]
+    digital_params = [layers[1].adapters.A, layers[1].adapters.B, norm.gamma, norm.beta, layers[0].adapters.A, layers[0].adapters.B]
+    before, weights = [p.clone() for p in digital_params], [L.W.clone() for L in layers]
+    net.train_step(x, labels, 0.5)
+    calls = net.ops.calls
+    assert [c[0] for c in calls] == ["fwd", "adapter_fwd", "gn_fwd", "fwd", "adapter_fwd", "bwd", "adapter_bwd", "gn_bwd", "adapter_bwd", "clip_sgd"]
+    assert all(torch.equal(L.W, w) for L, w in zip(layers, weights))
+    (_, given, (y, T)), (_, gn_given, (z, mean, invstd)) = calls[1], calls[2]
+    assert torch.equal(given[1], calls[0][2]) and torch.equal(gn_given[0], y) and torch.equal(calls[3][1][2], z)
+    assert torch.equal(calls[6][1][1], calls[5][2]) and torch.equal(calls[7][1][1], calls[6][2][0])   # dX in place on the crossbar's error
+    rows = np.array([0, 1, 2, -1] * 6)
+    for k in (6, 8):
+        _, (plan, base, dY, X, T, A, B, scale), (dX, dA, dB) = calls[k]
+        want = digital.adapter_bwd(rows, np.zeros(X.shape), host(dY), host(X), host(T), host(A), host(B), host(scale))
+        for got, w in ((dA, want[1]), (dB, want[2])):
+            assert np.abs(host(got) - w).max() <= 1e-5 * np.abs(w).max()              # (60-term sums: some 2^-20 of their size)
+    params, grads, lr, most = calls[9][1]
+    assert [g.shape for g in grads] == [p.shape for p in digital_params] and torch.equal(grads[2], calls[7][2][1])
+    size = digital.grad_norm([host(g) for g in grads])
+    assert size > most and abs(float(net.grad_norm.cpu()[0]) - size) <= 1.01 * U * size
+    for p, b, g in zip(digital_params, before, grads):
+        step = lr * most / size * host(g)
+        within(p, host(b) - step, U * (np.abs(host(b)) + 6 * np.abs(step)), "parameter")
+
+
+def test_serving_with_compact_adapters(xb):
+    """bfloat16 adapters give what their rounded values give, and a row without an adapter what the crossbars give."""
+    net, x, labels = perceptron(xb)
+    for L in net.layers:
+        L.adapters.compact()
+    got = net.forward(x, 0)
+    for L in net.layers:
+        L.adapters.A, L.adapters.B = L.adapters.A.float(), L.adapters.B.float()
+    assert torch.equal(got, net.forward(x, 0))
+    net.set_requests(None)
+    plain = net.forward(x, 0)
+    assert torch.equal(got[3::4], plain[3::4]) and not torch.equal(got, plain)
+
+
+@pytest.mark.parametrize("kind", ["perceptron", "residual"])
+def test_frozen_steps_from_a_hip_graph(xb, kind):
+    def make():
+        if kind == "perceptron":
+            return perceptron(xb)
+        import workloads
+        from paper_2002_11151_amd import resnet_cifar
+        net = resnet_cifar.ResNetCifar(workloads.config_kwargs("resnet20"), batch=4, n_blocks=1, image=8, classes=10, widths=(16, 32, 64), seed=1,
+                                       norm="group", groups=4)
+        gen = torch.Generator(device="cuda")
+        gen.manual_seed(5)
+        x, labels = torch.randn((4, 8, 8, 3), generator=gen, device="cuda"), torch.arange(4, device="cuda").to(torch.int32)
+        net.calibrate(x, labels)
+        net.frozen, net.max_grad_norm = True, 0.5
+        net.add_adapters(2, 5)
+        net.set_requests(dev([1, 0, -1, 1], np.int32))
+        return net, x, labels
+    (eager, x, labels), (graphed, _, _) = make(), make()
+    batches = [x, x * 0.5, x * 0.75, x * 0.25]
+    want = [eager.train_step(b, labels, 0.02).clone() for b in batches]
+    norms = float(eager.grad_norm.cpu()[0])
+    got = [graphed.capture(batches[0], labels, 0.02).clone()]
+    for b in batches[1:]:
+        torch.cuda.synchronize()
+        got.append(graphed.replay(b, labels).clone())
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and float(graphed.grad_norm.cpu()[0]) == norms > 0
+    for a, b in zip(eager.layers, graphed.layers):
+        assert torch.equal(a.W, b.W)
+        if a.adapters is not None:
+            assert torch.equal(a.adapters.A, b.adapters.A) and torch.equal(a.adapters.B, b.adapters.B) and b.adapters.B.any()
