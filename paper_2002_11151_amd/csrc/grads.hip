@@ -34,7 +34,7 @@ static_assert(sizeof(Table) + 64 <= 4096, "kernel arguments");
 struct Piece {
   int tensor;
   size_t from, to;
-  __device__ __forceinline__ Piece(const Table& t, uint32_t chunk) {
+  __device__ __forceinline__ Piece(const Table& t, uint32_t chunk, size_t each = kChunk) {
     int lo = 0, hi = t.tensors - 1;    // the last tensor with first <= chunk (tensors without elements have no chunk)
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
@@ -42,8 +42,8 @@ struct Piece {
       else hi = mid - 1;
     }
     tensor = lo;
-    from = (size_t)(chunk - t.first[lo]) * kChunk;
-    to = from + kChunk < t.n[lo] ? from + kChunk : (size_t)t.n[lo];
+    from = (size_t)(chunk - t.first[lo]) * each;
+    to = from + each < t.n[lo] ? from + each : (size_t)t.n[lo];
   }
 };
 
@@ -60,6 +60,44 @@ __device__ __forceinline__ double block_sum(double s, double (&red)[4]) {
 __device__ __forceinline__ void add_squares(double& s, const f4& v) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) s = __builtin_fma((double)v[e], (double)v[e], s);
+}
+
+// The norm of a few short tensors in one launch: one block, a wave takes every sixteenth piece of 1024 elements.
+constexpr size_t kShort = 65536;       // elements in all
+constexpr size_t kPiece = 1024;
+__global__ __launch_bounds__(1024) void norm_short_kernel(const Table t, float* norm) {
+  __shared__ double red[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  double s = 0.0;
+  for (uint32_t piece = wave; piece < t.first[t.tensors]; piece += 16) {
+    const Piece at(t, piece, kPiece);
+    const float* g = t.g[at.tensor] + at.from;
+    const int n = (int)(at.to - at.from);
+    f4 v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = 256 * u + 4 * lane;
+      v[u] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+      if (i + 3 < n) {
+        v[u] = *reinterpret_cast<const f4*>(g + i);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+          if (i + e < n) v[u][e] = g[i + e];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) add_squares(s, v[u]);
+  }
+#pragma unroll
+  for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d, 64);
+  if (lane == 0) red[wave] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    s = 0.0;
+    for (int w = 0; w < 16; ++w) s += red[w];
+    norm[0] = (float)::sqrt(s);
+  }
 }
 
 __global__ __launch_bounds__(256) void norm_partial_kernel(const Table t, double* part) {
@@ -210,13 +248,14 @@ struct Launches {
   const float* const* grads;
   const size_t* sizes;
   int tensors, next = 0;
+  size_t each = kChunk;
   Table t;
   unsigned blocks = 0;
   bool more() {
     t.tensors = 0;
     t.first[0] = 0;
     while (next < tensors && t.tensors < kTensors) {
-      const size_t chunks = (sizes[next] + kChunk - 1) / kChunk;
+      const size_t chunks = (sizes[next] + each - 1) / each;
       if (chunks) {
         t.g[t.tensors] = grads[next];
         t.p[t.tensors] = const_cast<float*>(params ? params[next] : grads[next]);
@@ -274,6 +313,13 @@ int xbar_grad_norm(const float* const* grads, const size_t* sizes, int tensors, 
   if (rc) return rc;
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   double* part = reinterpret_cast<double*>(ws);
+  size_t total = 0;
+  for (int i = 0; i < tensors; ++i) total += sizes[i];
+  Launches l{nullptr, grads, sizes, tensors, 0, kPiece};
+  if (total <= kShort && tensors <= kTensors && l.more()) {
+    hipLaunchKernelGGL(norm_short_kernel, dim3(1), dim3(1024), 0, st, l.t, norm);
+    return launched();
+  }
   int parts;
   if (partial_sums(Launches{nullptr, grads, sizes, tensors}, part, &parts, st)) return XBAR_EHIP;
   hipLaunchKernelGGL(norm_final_kernel, dim3(1), dim3(256), 0, st, part, parts, norm);
