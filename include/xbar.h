@@ -386,7 +386,8 @@ int xbar_absmax(const float* x, size_t n, float* result, void* ws, size_t ws_byt
  *            with skip)
  *   act      XBAR_ACT_*; a ReLU's output and gradient are 0 where z is not above 0 (NaN too), as in relu_fwd
  * skip (shape of x) may be NULL.  Outputs must not overlap inputs (XBAR_EINVAL for y, dx and dskip).  Statistics are accumulated in
- * double precision in a fixed order.  ws: xbar_gn_workspace_bytes; channels <= 2^20, batch groups < 2^25, else XBAR_ESHAPE.
+ * double precision in a fixed order.  ws: xbar_gn_workspace_bytes; channels <= 2^20, batch groups < 2^23 (2^25
+ * for groups of up to 1024 values), batch positions < 2^32 / 32, else XBAR_ESHAPE.
  */
 #define XBAR_ACT_NONE 0
 #define XBAR_ACT_RELU 1
@@ -436,7 +437,7 @@ int xbar_adapter_bwd(const void* plan, size_t plan_bytes, const float* base, con
  *   clip_sgd   the same norm, then p <- p - lr (c g) with the bits of grad_clip and sgd, but the gradients stay as they are.
  *              max_norm = INFINITY: c is 1
  * The squares are summed in double precision in a fixed order; norm is rounded to float at the end.  Where a gradient is infinite or NaN the
- * norm says so and nothing else is written.  What is written (the gradients of grad_clip, the parameters of clip_sgd, norm, ws) must
+ * norm says so and nothing else is written.  What is written (norm, ws, the gradients of grad_clip, the parameters of clip_sgd) must
  * not overlap itself or anything that is read: XBAR_EINVAL.  ws: xbar_grads_workspace_bytes(tensors).
  */
 #define XBAR_GRADS_MAX_TENSORS 2048

@@ -222,23 +222,21 @@ int checked(const float* const* params, const float* const* grads, const size_t*
   }
   if (!norm || (reinterpret_cast<uintptr_t>(norm) & 15u) || !ws || (reinterpret_cast<uintptr_t>(ws) & 15u)) return XBAR_EALIGN;
   if (ws_bytes < xbar_grads_workspace_bytes(tensors)) return XBAR_EWORKSPACE;
-  if (writes) {
-    Range ranges[2 * XBAR_GRADS_MAX_TENSORS + 2];
-    int n = 0;
-    const uintptr_t to_norm = reinterpret_cast<uintptr_t>(norm), to_ws = reinterpret_cast<uintptr_t>(ws);
-    ranges[n++] = Range{to_norm, to_norm + sizeof(float), 1};
-    ranges[n++] = Range{to_ws, to_ws + xbar_grads_workspace_bytes(tensors), 1};
-    for (int i = 0; i < tensors; ++i) {
-      if (!sizes[i]) continue;
-      const uintptr_t g = reinterpret_cast<uintptr_t>(grads[i]);
-      ranges[n++] = Range{g, g + 4 * sizes[i], params == nullptr};
-      if (params) {
-        const uintptr_t p = reinterpret_cast<uintptr_t>(params[i]);
-        ranges[n++] = Range{p, p + 4 * sizes[i], 1};
-      }
+  Range ranges[2 * XBAR_GRADS_MAX_TENSORS + 2];
+  int n = 0;
+  const uintptr_t to_norm = reinterpret_cast<uintptr_t>(norm), to_ws = reinterpret_cast<uintptr_t>(ws);
+  ranges[n++] = Range{to_norm, to_norm + sizeof(float), 1};
+  ranges[n++] = Range{to_ws, to_ws + xbar_grads_workspace_bytes(tensors), 1};
+  for (int i = 0; i < tensors; ++i) {
+    if (!sizes[i]) continue;
+    const uintptr_t g = reinterpret_cast<uintptr_t>(grads[i]);
+    ranges[n++] = Range{g, g + 4 * sizes[i], writes && !params};
+    if (params) {
+      const uintptr_t p = reinterpret_cast<uintptr_t>(params[i]);
+      ranges[n++] = Range{p, p + 4 * sizes[i], 1};
     }
-    if (written_twice(ranges, n)) return XBAR_EINVAL;
   }
+  if (written_twice(ranges, n)) return XBAR_EINVAL;
   return XBAR_OK;
 }
 

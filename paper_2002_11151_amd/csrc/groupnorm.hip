@@ -558,11 +558,15 @@ struct Plan {
   size_t bytes() const { return align256(sums() * sizeof(double)) + align256((size_t)s.batch * s.groups * 2 * sizeof(double)); }
 };
 
-// The limits on a shape: elements below 2^38, blocks of a launch below 2^24.
+// The limits on a shape: elements below 2^38, threads of a launch below 2^32.
 int shape_ok(int batch, int positions, int channels, int groups) {
   if (batch <= 0 || positions <= 0 || channels <= 0 || groups <= 0 || channels % groups) return XBAR_ESHAPE;
   if ((double)batch * positions * channels >= 274877906944.0 || channels > (1 << 20) || (double)batch * groups >= 33554432.0) return XBAR_ESHAPE;
-  return (double)batch * Plan(batch, positions, channels, groups).s.chunks >= 16777216.0 ? XBAR_ESHAPE : XBAR_OK;
+  const Plan p(batch, positions, channels, groups);
+  double threads = 256.0 * batch * p.s.chunks;
+  for (const bool backward : {false, true})
+    if (const int team = p.team(backward)) threads = std::max(threads, (double)p.held_grid(team).x * team_block(team));
+  return threads >= 4294967296.0 ? XBAR_ESHAPE : XBAR_OK;
 }
 
 template <template <int, int, int> class LAUNCH, class... ARGS>

@@ -76,7 +76,7 @@ def test_group_norm_refusals(xb):
         return lib.xbar_gn_fwd(a["x"], a["gamma"], a["beta"], a["skip"], a["y"], a["mean"], a["invstd"], a["batch"], a["positions"], a["channels"],
                                a["groups"], a["eps"], a["act"], a["ws"], a["n"], None)
     assert fwd(batch=0) == fwd(positions=0) == fwd(channels=0) == fwd(groups=0) == fwd(groups=5) == fwd(groups=24) == -2
-    assert fwd(batch=1 << 24, groups=1) == fwd(batch=1 << 20, positions=1 << 16) == fwd(channels=(1 << 20) + 3) == -2
+    assert fwd(batch=1 << 24, groups=1) == fwd(batch=1 << 20, positions=1 << 18) == fwd(batch=1 << 22, positions=2048) == fwd(channels=(1 << 20) + 3) == -2
     assert fwd(x=None) == fwd(gamma=P + 4) == fwd(skip=P + 8) == fwd(y=None) == fwd(mean=None) == fwd(ws=P + 1) == -3
     assert fwd(eps=-1.0) == fwd(eps=float("nan")) == fwd(act=3) == fwd(act=-1) == -1
     assert fwd(y=P) == fwd(y=P + 16) == fwd(skip=2 * big + 16) == -1
@@ -147,6 +147,7 @@ def test_gradient_list_refusals(xb):
     assert step(p=lists((3 * P, 0), (4 * P + 8, 0))[0]) == -3
     assert norm(n=n - 1) == clip(n=0) == step(n=n - 1) == -4
     assert clip(most=0.0) == clip(most=float("nan")) == clip(most=-1.0) == step(most=0.0) == step(lr=float("inf")) == step(lr=float("nan")) == -1
+    assert norm(out=P) == norm(ws=2 * P - 16) == norm(out=2 * far) == -1
     # the same memory twice: among the gradients that are scaled, the parameters, parameters and gradients, results and workspace
     assert clip(g=lists((P, 0), (P, 0))[0]) == clip(g=lists((P, 0), (P - 16, 0))[0]) == clip(out=P) == clip(ws=P) == -1
     assert step(p=lists((3 * P, 0), (3 * P, 0))[0]) == step(p=lists((3 * P, 0), (2 * P + 16, 0))[0]) == step(out=3 * P) == step(ws=P) == -1

@@ -466,3 +466,44 @@ def test_frozen_steps_from_a_hip_graph(xb, kind):
         assert torch.equal(a.W, b.W)
         if a.adapters is not None:
             assert torch.equal(a.adapters.A, b.adapters.A) and torch.equal(a.adapters.B, b.adapters.B) and b.adapters.B.any()
+
+
+# ---- beyond 32 bits --------------------------------------------------------------------------------
+def test_elements_beyond_32_bits(xb):
+    """Tensors of more than 2^31 elements: what lies at their end is right (compared there, in float64, with the same chains' bounds)."""
+    for shape, groups in (((3, 12_000_000, 64), 4), ((2_200_000, 1, 1024), 1)):    # sums in three launches; groups in registers
+        C = shape[-1]
+        ones, zeros = torch.ones(C, device="cuda"), torch.zeros(C, device="cuda")
+        x = torch.empty(shape, device="cuda").normal_()
+        assert x.numel() > 2 ** 31
+        y, mean, invstd = xb.gn_fwd(x, ones, zeros, groups)
+        part = x[-1:, -1000:].cpu().numpy()
+        want = torch.stack([x[-1].reshape(-1, groups, C // groups)[:, g].double().mean() for g in range(groups)]).cpu().numpy()
+        assert np.abs(host(mean[-1]) - want).max() <= 2 * U * np.abs(want).max() + 1e-12
+        z = digital.gn_z(part, np.ones(C), np.zeros(C), host(mean[-1:]), host(invstd[-1:]))[1]
+        within(y[-1:, -1000:], z, 1.01 * U * np.abs(z) + 1e-13)
+        dx = xb.gn_bwd(x, y, ones, zeros, mean, invstd)[0]
+        assert float(dx[-1, -1000:].abs().max()) < 1e-2                              # the error along y itself is taken out of dx (eps is left)
+        del x, y, dx
+    M, K = 40_000, 60_000
+    X = torch.empty((M, K), device="cuda").normal_()
+    assert X.numel() > 2 ** 31
+    rows = (torch.arange(M, device="cuda") % 3 - 1).to(torch.int32)
+    A, B, scale = torch.randn((2, 2, K), device="cuda"), torch.randn((2, 2, 8), device="cuda"), torch.ones(2, device="cuda")
+    base = torch.randn((M, 8), device="cuda")
+    plan = xb.adapter_plan(rows, 2)
+    Y, T = xb.adapter_fwd(plan, base, X, A, B, scale)
+    tail = slice(M - 6, M)
+    c = [t.cpu().numpy() for t in (rows[tail], base[tail], X[tail], A, B, scale)]
+    want, T64 = digital.adapter_fwd(*c)
+    sizes, aT = digital.adapter_fwd(c[0], np.zeros_like(want), *[np.abs(t) for t in c[2:]])
+    within(T[tail], T64, (K / 4 + 48) * U * aT + 1e-30)
+    within(Y[tail], want, (K / 4 + 60) * U * sizes + 2 * U * (np.abs(c[1]) + np.abs(want)))
+    dX = xb.adapter_bwd(plan, X, Y, X[:, :].clone(), T, A, B, scale)[0]
+    dXw = digital.adapter_bwd(c[0], c[2], host(Y[tail]), c[2], host(T[tail]), c[3], c[4], c[5])[0]
+    size = digital.adapter_bwd(c[0], np.zeros_like(dXw), np.abs(host(Y[tail])), c[2], host(T[tail]), np.abs(c[3]), np.abs(c[4]), c[5])[0]
+    within(dX[tail], dXw, 60 * U * size + 2 * U * (np.abs(c[2]) + np.abs(dXw)))
+    flat = X.reshape(-1)
+    flat.zero_()
+    flat[-1], flat[2 ** 31 + 5], flat[3] = 3.0, 4.0, 12.0
+    assert float(xb.grad_clip([flat], 6.5).cpu()[0]) == 13.0 and float(flat[-1]) == 1.5 and float(flat[2 ** 31 + 5]) == 2.0
