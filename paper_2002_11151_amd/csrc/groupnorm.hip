@@ -1,7 +1,8 @@
 // Group normalisation with an activation, channels last: the normalisation of a digital peripheral that needs no batch -- statistics
 // per sample and group of neighbouring channels -- so that a network runs one request, or trains on small batches.
 //   z = gamma (x - mean) invstd + beta (+ skip),  y = act(z)
-// Evaluated in double precision up to z, rounded once.  HBM-bound elementwise and reduction work.
+// Evaluated in double precision up to z, rounded once.  HBM-bound elementwise and reduction work: 64 x 56 x 56 x 256 with a skip takes 39 us for the
+// sums (5.3 TB/s), 5 for the statistics and 110 for the values (5.6 TB/s); 64 x 28 x 28 x 512 backward 80 us in one pass (3.9 TB/s).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -217,7 +218,9 @@ __global__ __launch_bounds__(team_block(TEAM)) void gn_held_fwd_kernel(const flo
     }
 }
 
-// Backward: q divides TEAM, so that a thread's elements all lie in the same channels.  sums[sample][channel][2]: sums of g and of g xhat over the
+// Backward: only the errors stay in registers; x is read again for dx, from the caches, and four vectors of each tensor are on their way at a
+// time, so that a compute unit holds two blocks of 512 threads (64 x 28 x 28 x 512: 92 us with both tensors held in 166 registers, 84.5 with 110).
+// q divides TEAM, so that a thread's elements all lie in the same channels.  sums[sample][channel][2]: sums of g and of g xhat over the
 // positions; with one sample they are dbeta and dgamma themselves and go there.
 template <int ACT, int VEC, int TEAM, int N>
 __global__ __launch_bounds__(team_block(TEAM)) void gn_held_bwd_kernel(const float* x, const float* dy, const float* gamma, const float* beta,
@@ -232,13 +235,7 @@ __global__ __launch_bounds__(team_block(TEAM)) void gn_held_bwd_kernel(const flo
   const int count = mine ? s.positions * q : 0, t = threadIdx.x % TEAM, row = t / q, c = t - row * q, dr = TEAM / q;
   const int c0 = g * s.per_group;
   const size_t from = (size_t)b * s.positions * s.channels + (size_t)row * s.channels + c0 + c * VEC, step = (size_t)dr * s.channels;
-  float v[N][VEC], d[N][VEC];
-#pragma unroll
-  for (int j = 0; j < N; ++j)
-    if (t + TEAM * j < count) {
-      load_vec<VEC>(x + from + j * step, v[j]);
-      load_vec<VEC>(dy + from + j * step, d[j]);
-    }
+  float d[N][VEC];
   float ga[VEC], be[VEC];
   load_vec<VEC>(gamma + c0 + c * VEC, ga);
   load_vec<VEC>(beta + c0 + c * VEC, be);
@@ -250,19 +247,30 @@ __global__ __launch_bounds__(team_block(TEAM)) void gn_held_bwd_kernel(const flo
 #pragma unroll
   for (int i = 0; i < VALUES; ++i) p[i] = 0.0;
 #pragma unroll
-  for (int j = 0; j < N; ++j)
-    if (t + TEAM * j < count) {
-      float k[VEC];
-      if (ACT != XBAR_ACT_NONE && skip) load_vec<VEC>(skip + from + j * step, k);
+  for (int j0 = 0; j0 < N; j0 += 4) {
+    float v[4][VEC];
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        double z = nm[e].z(v[j][e]);
-        if (ACT != XBAR_ACT_NONE && skip) z += (double)k[e];
-        d[j][e] = act_bwd<ACT>(z, d[j][e]);
-        p[2 * e] += (double)d[j][e];
-        p[2 * e + 1] = __builtin_fma((double)d[j][e], (double)v[j][e], p[2 * e + 1]);
+    for (int j = j0; j < j0 + 4 && j < N; ++j)
+      if (t + TEAM * j < count) {
+        load_vec<VEC>(x + from + j * step, v[j - j0]);
+        load_vec<VEC>(dy + from + j * step, d[j]);
       }
-    }
+#pragma unroll
+    for (int j = j0; j < j0 + 4 && j < N; ++j)
+      if (t + TEAM * j < count) {
+        float k[VEC];
+        if (ACT != XBAR_ACT_NONE && skip) load_vec<VEC>(skip + from + j * step, k);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          double z = nm[e].z(v[j - j0][e]);
+          if (ACT != XBAR_ACT_NONE && skip) z += (double)k[e];
+          d[j][e] = act_bwd<ACT>(z, d[j][e]);
+          p[2 * e] += (double)d[j][e];
+          p[2 * e + 1] = __builtin_fma((double)d[j][e], (double)v[j - j0][e], p[2 * e + 1]);
+        }
+      }
+    __builtin_amdgcn_sched_barrier(0);
+  }
   // Over the lanes with the same channels: every level exchanges half of what is left and keeps the other half, so that a lane ends up with
   // VALUES >> levels of the sums (or one, which several hold).
   int left = VALUES, which = 0;
@@ -318,13 +326,15 @@ __global__ __launch_bounds__(team_block(TEAM)) void gn_held_bwd_kernel(const flo
 #pragma unroll
   for (int j = 0; j < N; ++j)
     if (t + TEAM * j < count) {
-      float o[VEC];
+      float o[VEC], again[VEC];
+      load_vec<VEC>(x + from + j * step, again);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        o[e] = sl[e].dx(d[j][e], v[j][e]);
+        o[e] = sl[e].dx(d[j][e], again[e]);
       }
       store_vec<VEC>(dx + from + j * step, o);
       if (dskip) store_vec<VEC>(dskip + from + j * step, d[j]);
+      if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);
     }
 }
 
@@ -540,7 +550,7 @@ struct Plan {
   // Threads that hold a group (0: too large, three launches instead).  Few threads where a few vectors each are enough, so that small groups
   // share a block; 512 with eight vectors each at most: with 16 a block fills a compute unit and nothing hides its loads (64 x 56 x 56 x 256 in
   // 32 groups, forward: 219 us, 200 with 1024 threads, against 167 in three launches).  us, held / three launches: forward 13 x 255 x 90 in 9
-  // groups 15.1 / 19.9, 1 x 64 x 64 14.9 / 19.0; backward 128 x 1024 x 16 in 4 groups 18.5 / 24, 64 x 784 x 512 in 32 92 / 107.
+  // groups 15.1 / 19.9, 1 x 64 x 64 14.9 / 19.0; backward 128 x 1024 x 16 in 4 groups 17.4 / 24, 64 x 784 x 512 in 32 84.5 / 107.
   int team(bool backward) const {
     const int q = s.per_group / held_vec, most = 512 * 8;
     if (elements > most) return 0;
