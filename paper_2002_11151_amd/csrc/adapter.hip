@@ -83,12 +83,32 @@ inline size_t plan_layout(void* base, int M, int adapters, PlanAt* at) {
 
 __device__ __forceinline__ int bin_of(int id, int adapters) { return (unsigned)id < (unsigned)adapters ? id : adapters; }
 
+// Bins of rows m .. m + 3, -1 beyond M.
+__device__ __forceinline__ int4 bins_of(const int32_t* rows, int m, int M, int adapters) {
+  int4 v = make_int4(-1, -1, -1, -1);
+  if (m + 3 < M) {
+    const int4 id = *reinterpret_cast<const int4*>(rows + m);
+    v = make_int4(bin_of(id.x, adapters), bin_of(id.y, adapters), bin_of(id.z, adapters), bin_of(id.w, adapters));
+  } else {
+    if (m < M) v.x = bin_of(rows[m], adapters);
+    if (m + 1 < M) v.y = bin_of(rows[m + 1], adapters);
+    if (m + 2 < M) v.z = bin_of(rows[m + 2], adapters);
+  }
+  return v;
+}
+
 // Rows of every adapter (bin `adapters`: rows without one), one wave per bin over all rows.
 __global__ __launch_bounds__(256) void plan_count_kernel(const int32_t* rows, int M, int adapters, PlanAt p) {
   const int bin = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (bin > adapters) return;
   int n = 0;
-  for (int m = lane; m < M; m += 64) n += bin_of(rows[m], adapters) == bin;
+  for (int m0 = 0; m0 < M; m0 += 2048) {                        // eight loads in flight
+    int4 id[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) id[u] = bins_of(rows, m0 + 256 * u + 4 * lane, M, adapters);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) n += (id[u].x == bin) + (id[u].y == bin) + (id[u].z == bin) + (id[u].w == bin);
+  }
 #pragma unroll
   for (int d = 32; d; d >>= 1) n += __shfl_xor(n, d, 64);
   if (lane == 0) p.start[bin] = n;
@@ -162,17 +182,33 @@ __global__ __launch_bounds__(256) void plan_place_kernel(const int32_t* rows, in
   if (begin == end) return;
   int at = begin, last = 0;
   int* padded = p.rows + (size_t)p.tile0[bin] * kTileRows;
-  for (int m0 = 0; m0 < M; m0 += 64) {
-    const int m = m0 + lane;
-    const bool mine = m < M && bin_of(rows[m], adapters) == bin;
-    const unsigned long long all = __ballot(mine);
-    if (mine) {
-      const int place = at + __popcll(all & ((1ull << lane) - 1));
-      p.perm[place] = m;
-      padded[place - begin] = m;
+  const unsigned long long below = (1ull << lane) - 1;
+  for (int m0 = 0; m0 < M; m0 += 2048) {
+    int4 id[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) id[u] = bins_of(rows, m0 + 256 * u + 4 * lane, M, adapters);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int four[4] = {id[u].x, id[u].y, id[u].z, id[u].w}, m = m0 + 256 * u + 4 * lane;
+      unsigned long long all[4];
+      int place = at;                                           // behind all of the lanes before
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        all[e] = __ballot(four[e] == bin);
+        place += __popcll(all[e] & below);
+        at += __popcll(all[e]);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (four[e] == bin) {
+          p.perm[place] = m + e;
+          padded[place - begin] = m + e;
+          ++place;
+        }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (all[e]) last = max(last, m0 + 256 * u + 4 * (63 - __clzll(all[e])) + e);
     }
-    if (all) last = m0 + 63 - __clzll(all);
-    at += __popcll(all);
   }
   const int odd = (end - begin) % kTileRows;
   if (odd && lane < kTileRows - odd) padded[end - begin + lane] = last;
