@@ -315,7 +315,6 @@ __device__ __forceinline__ bool planned(const PlanAt& p, int M, int adapters) {
 }
 
 // ---- the products ----------------------------------------------------------------------------------
-__device__ __forceinline__ float wide(float x) { return x; }
 __device__ __forceinline__ float wide(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }   // bfloat16
 
 // The base passes through once and should not take the caches' room.  (The output is stored the ordinary way: 4096 x 4096 values and a ReLU
