@@ -277,6 +277,8 @@ class Network:
     grad_norm = None   # the norm that their gradients had in the last such step (device tensor)
     _pending = ()     # (parameter, gradient) pairs of the step so far
     requests = None   # plan of the batch's adapters (set_requests)
+    _plan = _graph_plan = None   # the plan whose buffer the next one of its size is written into; the one a captured step reads
+    _graph_tensors = ()   # what a captured step knows of the adapters, by address
     norm_bytes = 0    # workspace of the widest group normalisation
     pair_devices = False   # aggregate updates keep the positive and the negative device of a weight as states of their own
 
@@ -318,8 +320,25 @@ class Network:
         self.adapter_count = count
 
     def set_requests(self, rows):
-        """The adapter of every row of the next batches (int32 tensor; none: a negative number), or None: no adapters."""
-        self.requests = None if rows is None else self.ops.adapter_plan(rows, self.adapter_count)
+        """The adapter of every row of the next batches (int32 tensor; none: a negative number), or None: no adapters.  On the stream of the
+        steps: the plan of as many rows and adapters as before is written in place, where a captured step reads it -- its replays
+        follow the requests too, as long as there are requests and as many rows as at its capture."""
+        if rows is None:
+            self.requests = None
+            return
+        for plan in (self._graph_plan, self._plan):
+            if plan is not None and (plan.rows, plan.adapters) == (rows.shape[0], self.adapter_count):
+                self.requests = self._plan = self.ops.adapter_plan(rows, self.adapter_count, buffer=plan.buffer)
+                return
+        self.requests = self._plan = self.ops.adapter_plan(rows, self.adapter_count)
+
+    def _adapter_tensors(self):
+        """What kernels of this batch know of the adapters, by address: the plan, every layer's parameters.  (Tensors of their own on
+        the same memory, which stays as long as they do.)"""
+        if self.requests is None:
+            return ()
+        own = [t for L in self.layers if L.adapters is not None for t in (L.adapters.A, L.adapters.B, L.adapters.scale)]
+        return tuple(t.detach() for t in (self.requests.buffer, *own))
 
     def train_step(self, x, labels, lr):
         """One SGD step on a batch: returns the per-sample losses (device tensor)."""
@@ -355,6 +374,7 @@ class Network:
             self._graph = torch.cuda.CUDAGraph()
             with torch.cuda.graph(self._graph, stream=side):
                 self._graph_loss = self._counted_step(lr)
+            self._graph_plan, self._graph_tensors = self.requests, self._adapter_tensors()
         finally:
             xb.set_step_source(None)
         self.step_no += 1
@@ -362,7 +382,11 @@ class Network:
 
     def replay(self, x, labels):
         """The next training step from the captured graph; returns the per-sample losses (a buffer that the next
-        replay overwrites)."""
+        replay overwrites).  The requests of the batch may be other ones than at the capture (set_requests), not another number
+        of them, and the adapters have to be the captured ones (ValueError)."""
+        if [t.data_ptr() for t in self._adapter_tensors()] != [t.data_ptr() for t in self._graph_tensors]:
+            raise ValueError("replay(): requests or adapters are no longer those that the captured step reads (switched on or off, another "
+                             "number of rows, new or compacted adapters); capture the step again")
         self._graph_x.copy_(x)
         self._graph_labels.copy_(labels)
         self._graph.replay()

@@ -320,3 +320,102 @@ def test_normalisations_of_the_residual_networks(xb):
             _network(xb, [("flatten",), ("fc", 20), ("groupnorm", 3, "relu"), ("fc", 5)])
     finally:
         resnet_cifar.Network.ops = xb
+
+
+# ---- captured steps --------------------------------------------------------------------------------
+@pytest.fixture()
+def no_graphs(monkeypatch):
+    """capture() and replay() without a GPU: the two passes of a capture run one after another, a replay launches nothing."""
+    import contextlib
+    import torch
+
+    class Nothing:
+        def __init__(self, *a, **k):
+            pass
+
+        def wait_stream(self, other):
+            pass
+
+        def replay(self):
+            pass
+    from paper_2002_11151_amd import xbar
+    for name in ("Stream", "CUDAGraph"):
+        monkeypatch.setattr(torch.cuda, name, Nothing)
+    for name in ("stream", "graph"):
+        monkeypatch.setattr(torch.cuda, name, lambda *a, **k: contextlib.nullcontext())
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: Nothing())
+    monkeypatch.setattr(xbar, "set_step_source", lambda counter: None)
+
+
+def _adapted(xb, spec=None, requests=(0, 1, -1, 1, 0, 0)):
+    """A frozen network with adapters whose plans lie in buffers, as the binding's."""
+    import torch
+    net, ops = _network(xb, SPEC if spec is None else spec)
+
+    class Planned(type(ops)):
+        def adapter_plan(self, rows, n, buffer=None):
+            self._log("adapter_plan", n=n)
+            buffer = rows.clone() if buffer is None else buffer.copy_(rows)
+            return xb.AdapterPlan(buffer, rows.shape[0], n)
+
+        def adapter_fwd(self, plan, *args, **kw):
+            self.planned = plan.buffer.data_ptr()
+            return super().adapter_fwd(plan.buffer, *args, **kw)
+
+        def adapter_bwd(self, plan, *args, **kw):
+            return super().adapter_bwd(plan.buffer, *args, **kw)
+
+        def step_advance(self, counter):
+            counter += 1
+    ops.__class__ = Planned
+    x, labels = _batch()
+    net.calibrate(x, labels)
+    net.frozen, net.max_grad_norm = True, 0.25
+    net.add_adapters(2, 3)
+    if requests is not None:
+        net.set_requests(torch.tensor(requests, dtype=torch.int32))
+    ops.calls.clear()
+    return net, ops, x, labels
+
+
+def test_requests_of_a_captured_step_are_planned_where_it_reads_them(xb, no_graphs):
+    import torch
+    net, ops, x, labels = _adapted(xb)
+    net.capture(x, labels, 0.1)
+    read = ops.planned
+    for rows in ([1] * 6, [-1, 0, 1, 0, 1, -1]):
+        net.set_requests(torch.tensor(rows, dtype=torch.int32))
+        assert net.requests.buffer.data_ptr() == read and net.requests.buffer.tolist() == rows
+        net.replay(x, labels)
+    # what a captured step cannot follow is refused, and its plan and adapters stay in memory
+    net.set_requests(None)
+    with pytest.raises(ValueError):
+        net.replay(x, labels)
+    net.set_requests(torch.tensor([0, 1], dtype=torch.int32))
+    assert net.requests.buffer.data_ptr() != read
+    with pytest.raises(ValueError):
+        net.replay(x, labels)
+    net.set_requests(torch.tensor([0, 0, 0, 0, 1, 1], dtype=torch.int32))       # the captured number again: back in its buffer
+    assert net.requests.buffer.data_ptr() == read
+    net.replay(x, labels)
+    net.add_adapters(2, 3)
+    with pytest.raises(ValueError):
+        net.replay(x, labels)
+    net.capture(x, labels, 0.1)
+    net.replay(x, labels)
+    for L in net.layers:
+        L.adapters.compact()
+    with pytest.raises(ValueError):
+        net.replay(x, labels)
+
+
+def test_requests_after_a_capture_without_them_are_refused(xb, no_graphs):
+    import torch
+    net, ops, x, labels = _adapted(xb, requests=None)
+    net.capture(x, labels, 0.1)
+    net.replay(x, labels)
+    net.set_requests(torch.tensor([0, 1, -1, 1, 0, 0], dtype=torch.int32))
+    with pytest.raises(ValueError):
+        net.replay(x, labels)
+    net.set_requests(None)
+    net.replay(x, labels)

@@ -507,3 +507,29 @@ def test_elements_beyond_32_bits(xb):
     flat.zero_()
     flat[-1], flat[2 ** 31 + 5], flat[3] = 3.0, 4.0, 12.0
     assert float(xb.grad_clip([flat], 6.5).cpu()[0]) == 13.0 and float(flat[-1]) == 1.5 and float(flat[2 ** 31 + 5]) == 2.0
+
+
+# ---- captured steps of networks --------------------------------------------------------------------
+def test_replays_follow_the_requests(xb):
+    """Other requests before every replay, memory of the plan's size taken in between: each replay is the eager step with those requests."""
+    (eager, x, labels), (graphed, _, _) = perceptron(xb), perceptron(xb)
+    rng = np.random.default_rng(11)
+    turns = [dev(rng.integers(-1, 3, size=24), np.int32) for _ in range(4)]
+    want = []
+    for rows in turns:
+        eager.set_requests(rows)
+        want.append(eager.train_step(x, labels, 0.2).clone())
+    graphed.set_requests(turns[0])
+    got, taken = [graphed.capture(x, labels, 0.2).clone()], []
+    for rows in turns[1:]:
+        graphed.set_requests(rows)
+        taken += [torch.full((n,), 1, dtype=torch.uint8, device="cuda") for n in (graphed.requests.buffer.numel(), 64, 4096)]
+        torch.cuda.synchronize()
+        got.append(graphed.replay(x, labels).clone())
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and not torch.equal(want[0], want[1])
+    for a, b in zip(eager.layers, graphed.layers):
+        assert torch.equal(a.adapters.A, b.adapters.A) and torch.equal(a.adapters.B, b.adapters.B)
+    graphed.set_requests(None)
+    with pytest.raises(ValueError):
+        graphed.replay(x, labels)
