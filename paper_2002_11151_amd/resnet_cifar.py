@@ -371,9 +371,11 @@ class Network:
             with torch.cuda.stream(side):
                 first = self._counted_step(lr).clone()
             main.wait_stream(side)
+            norm = self.grad_norm
             self._graph = torch.cuda.CUDAGraph()
             with torch.cuda.graph(self._graph, stream=side):
                 self._graph_loss = self._counted_step(lr)
+            self.grad_norm, self._graph_norm = norm, self.grad_norm        # the graph's own: not computed before the first replay
             self._graph_plan, self._graph_tensors = self.requests, self._adapter_tensors()
         finally:
             xb.set_step_source(None)
@@ -390,6 +392,7 @@ class Network:
         self._graph_x.copy_(x)
         self._graph_labels.copy_(labels)
         self._graph.replay()
+        self.grad_norm = self._graph_norm
         self.step_no += 1
         return self._graph_loss
 

@@ -419,3 +419,18 @@ def test_requests_after_a_capture_without_them_are_refused(xb, no_graphs):
         net.replay(x, labels)
     net.set_requests(None)
     net.replay(x, labels)
+
+
+def test_norm_of_a_captured_step_is_that_of_the_last_step(xb, no_graphs):
+    """capture() leaves the norm of the step that it ran, a replay the captured step's own, whatever eager steps came between."""
+    net, ops, x, labels = _adapted(xb)
+    norms, clip = [], ops.clip_sgd
+    ops.clip_sgd = lambda *a: norms.append(clip(*a)) or norms[-1]
+    net.capture(x, labels, 0.1)
+    assert len(norms) == 2 and net.grad_norm is norms[0]        # of the real step; the other one is the graph's, not yet computed
+    net.replay(x, labels)
+    assert net.grad_norm is norms[1]
+    net.train_step(x, labels, 0.1)
+    assert net.grad_norm is norms[2]
+    net.replay(x, labels)
+    assert net.grad_norm is norms[1]

@@ -533,3 +533,16 @@ def test_replays_follow_the_requests(xb):
     graphed.set_requests(None)
     with pytest.raises(ValueError):
         graphed.replay(x, labels)
+
+
+def test_norms_of_captured_steps(xb):
+    """net.grad_norm after the capture, after replays and after an eager step between them: that of the eager network's step."""
+    (eager, x, labels), (graphed, _, _) = perceptron(xb), perceptron(xb)
+    want, got = [], []
+    for step in (graphed.capture, None, None):
+        eager.train_step(x, labels, 0.2)
+        want.append(float(eager.grad_norm.cpu()[0]))
+        graphed.replay(x, labels) if step is None else step(x, labels, 0.2)
+        torch.cuda.synchronize()
+        got.append(float(graphed.grad_norm.cpu()[0]))
+    assert got == want and want[0] > 0
