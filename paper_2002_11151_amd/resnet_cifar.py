@@ -398,6 +398,7 @@ class Network:
 
     def _counted_step(self, lr):
         # the step argument is 0: the kernels add the device counter, which the last kernel of the step advances
+        self._pending = ()
         logits = self.forward(self._graph_x, 0)
         loss, dlogits = self.ops.softmax_xent(logits, self._graph_labels, 1.0 / self._graph_x.shape[0])
         self.backward(dlogits, 0, lr)

@@ -434,3 +434,10 @@ def test_norm_of_a_captured_step_is_that_of_the_last_step(xb, no_graphs):
     assert net.grad_norm is norms[2]
     net.replay(x, labels)
     assert net.grad_norm is norms[1]
+
+
+def test_capture_leaves_out_what_a_broken_step_left(xb, no_graphs):
+    net, ops, x, labels = _adapted(xb)
+    net._pending = ((x, x),)
+    net.capture(x, labels, 0.1)
+    assert [c[1]["tensors"] for c in ops.calls if c[0] == "clip_sgd"] == [6, 6]
