@@ -38,7 +38,7 @@ class CrossbarLayer:
         self.x_scale = self.g_scale = 1.0
         self.planes = torch.empty(xb.planes_bytes(self.cfg, K, N), dtype=torch.uint8, device=device)
         self.x = None
-        self.programmed = False            # the planes hold W as it is (only a frozen network asks)
+        self.programmed = None             # what the planes hold (_contents; only a frozen network asks)
         self.adapters = None               # low-rank adapters beside the projection (Network.add_adapters)
         self.profile = None                # stored wire distortion (with the profile flag), refreshed by forward()
         self.pair = None                   # (Gp, Gn) once the network updates the two devices of a weight separately
@@ -48,9 +48,11 @@ class CrossbarLayer:
         ops = self.net.ops
         if self.net.calibrating and self.net.adc_quantile is None:
             self.seen_x = self.x_scale = ops.absmax(x) or 1.0
-        if not (self.net.frozen and self.programmed):
+        if self.net.frozen:
+            self.keep_programmed(step, ws)
+        else:
             self._program(step, ws)
-        self.programmed = self.net.frozen
+            self.programmed = None
         self.x = x
         if self.net.adc_quantile is not None:
             self.cfg.adc_fs_fwd = self._measured_range(xb.OP_FWD, x, self.x_scale, self.cfg.xbar_rows, ws)
@@ -58,6 +60,17 @@ class CrossbarLayer:
             y = ops.fwd(self.cfg, self.planes, x, self.N, self.w_max, self.x_scale, ws=ws)
             return y if self._plan() is None else self.adapters.forward(self._plan(), y, x)
         return ops.conv_fwd(self.cfg, self.planes, x, self.geom, self.N, self.w_max, self.x_scale, ws=ws)
+
+    def _contents(self):
+        """The weights as a tensor and its count of writes through torch (tensors of the inference mode have none), and their range."""
+        return self.W, 0 if self.W.is_inference() else self.W._version, self.w_max
+
+    def keep_programmed(self, step, ws):
+        """In a frozen network: programs the planes where they do not hold these weights, or net.reprogram() asked for it."""
+        now, held = self._contents(), self.programmed
+        if held is None or held[0] is not now[0] or held[1:] != now[1:]:
+            self._program(step, ws)
+        self.programmed = now
 
     def _program(self, step, ws):
         ops = self.net.ops
@@ -272,7 +285,9 @@ class Network:
     fcm_every = 1         # with the stored-profile wire model: steps between two runs of the circuit-level model
     adc_quantile = None   # set while the converter ranges are being measured
     pulse = None     # dict(bl=slots per train, dw_min=state change per pulse): pulse-level updates of the crossbar layers
-    frozen = False   # the crossbars keep their conductances: programmed at the first forward pass, read ever after; digital parameters learn
+    # The crossbars keep their conductances: programmed at the first forward pass, read ever after; digital parameters learn.  Weights that torch
+    # writes (layer.W in place, or another tensor) are programmed at the next pass; after any other change: reprogram().
+    frozen = False
     max_grad_norm = None   # set: the digital parameters (normalisations, adapters) step together, their gradients clipped to this global norm
     grad_norm = None   # the norm that their gradients had in the last such step (device tensor)
     _pending = ()     # (parameter, gradient) pairs of the step so far
@@ -309,6 +324,11 @@ class Network:
         pending, self._pending = self._pending, ()
         if pending:
             self.grad_norm = self.ops.clip_sgd([p for p, _ in pending], [g for _, g in pending], lr, self.max_grad_norm)
+
+    def reprogram(self):
+        """The next pass of a frozen network programs its crossbars anew, with the variation of that step."""
+        for layer in self.layers:
+            layer.programmed = None
 
     def add_adapters(self, count, rank, scale=1.0, seed=0):
         """`count` low-rank adapters beside every fully connected layer; which row of a batch uses which: set_requests."""
@@ -389,6 +409,11 @@ class Network:
         if [t.data_ptr() for t in self._adapter_tensors()] != [t.data_ptr() for t in self._graph_tensors]:
             raise ValueError("replay(): requests or adapters are no longer those that the captured step reads (switched on or off, another "
                              "number of rows, new or compacted adapters); capture the step again")
+        if self.frozen:                    # the captured step reads the planes as they are
+            for layer in self.layers:
+                layer.keep_programmed(self.step_no, self.ws)
+        else:
+            self.reprogram()               # it writes the devices
         self._graph_x.copy_(x)
         self._graph_labels.copy_(labels)
         self._graph.replay()

@@ -441,3 +441,70 @@ def test_capture_leaves_out_what_a_broken_step_left(xb, no_graphs):
     net._pending = ((x, x),)
     net.capture(x, labels, 0.1)
     assert [c[1]["tensors"] for c in ops.calls if c[0] == "clip_sgd"] == [6, 6]
+
+
+# ---- frozen networks -------------------------------------------------------------------------------
+def test_weights_written_while_frozen_are_programmed(xb):
+    import torch
+    net, ops, x, labels = _adapted(xb)
+    first, second = net.layers
+
+    def tiles():
+        ops.calls.clear()
+        got = net.forward(x, 7)
+        return [c[1]["step"] for c in ops.calls if c[0] == "tile"], got
+    assert tiles()[0] == [7, 7] and tiles()[0] == []
+    before = tiles()[1]
+    first.W.mul_(0.5)                                             # in place
+    steps, after = tiles()
+    assert steps == [7] and not torch.equal(before, after) and tiles()[0] == []
+    second.W = second.W * 2                                       # another tensor
+    assert tiles()[0] == [7] and tiles()[0] == []
+    first.W.data.mul_(0.5)                                        # a write that torch does not count
+    net.reprogram()
+    assert tiles()[0] == [7, 7] and tiles()[0] == []
+    assert torch.equal(ops.programmed[first.planes.data_ptr()], first.W)
+    net.frozen = False
+    net.train_step(x, labels, 0.1)                                # the library writes W, which torch does not count either
+    net.frozen = True
+    assert tiles()[0] == [7, 7] and tiles()[0] == []
+
+
+def test_weights_without_a_count_of_writes(xb):
+    """A network made in inference mode: its tensors have no such count; programmed once, anew on demand."""
+    import torch
+    with torch.inference_mode():
+        net, ops, x, labels = _adapted(xb)
+        for _ in range(2):
+            net.forward(x, 0)
+        assert [c[0] for c in ops.calls].count("tile") == 2
+        net.reprogram()
+        net.forward(x, 0)
+        assert [c[0] for c in ops.calls].count("tile") == 4
+
+
+def test_replays_program_weights_written_while_frozen(xb, no_graphs):
+    net, ops, x, labels = _adapted(xb)
+    net.capture(x, labels, 0.1)
+    ops.calls.clear()
+    net.replay(x, labels)
+    assert not ops.calls
+    net.layers[1].W.mul_(0.5)
+    net.replay(x, labels)
+    assert [(c[0], c[1]["step"]) for c in ops.calls] == [("tile", 2)]
+    net.replay(x, labels)
+    assert len(ops.calls) == 1
+
+
+def test_replays_that_write_the_devices_leave_no_plane_valid(xb, no_graphs):
+    net, ops, x, labels = _adapted(xb)
+    net.frozen = False
+    net.capture(x, labels, 0.1)
+    net.frozen = True
+    net.forward(x, 0)
+    net.frozen = False
+    net.replay(x, labels)
+    net.frozen = True
+    ops.calls.clear()
+    net.forward(x, 0)
+    assert [c[0] for c in ops.calls].count("tile") == 2

@@ -546,3 +546,22 @@ def test_norms_of_captured_steps(xb):
         torch.cuda.synchronize()
         got.append(float(graphed.grad_norm.cpu()[0]))
     assert got == want and want[0] > 0
+
+
+def test_weights_loaded_into_a_frozen_network(xb):
+    """Weights written after the planes were programmed are what the next eager pass and the next replay run on."""
+    (eager, x, labels), (graphed, _, _) = perceptron(xb), perceptron(xb)
+    want, got = [eager.train_step(x, labels, 0.1).clone()], [graphed.capture(x, labels, 0.1).clone()]
+    for turn in range(2):
+        for net in (eager, graphed):
+            net.layers[turn].W.mul_(-0.75)
+        want.append(eager.train_step(x, labels, 0.1).clone())
+        torch.cuda.synchronize()
+        got.append(graphed.replay(x, labels).clone())
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    for a, b in zip(eager.layers, graphed.layers):
+        fresh = xb.tile(a.cfg, a.W, a.w_max, 1 + a.index)                       # layer 0 written before step 1, layer 1 before step 2
+        assert torch.equal(a.planes, b.planes)
+        dy = torch.randn((3, a.N), device="cuda")
+        assert torch.equal(xb.bwd(a.cfg, fresh, dy, a.K, a.w_max, 4.0), xb.bwd(a.cfg, a.planes, dy, a.K, a.w_max, 4.0))
