@@ -397,6 +397,7 @@ class Network:
                 self._graph_loss = self._counted_step(lr)
             self.grad_norm, self._graph_norm = norm, self.grad_norm        # the graph's own: not computed before the first replay
             self._graph_plan, self._graph_tensors = self.requests, self._adapter_tensors()
+            self._graph_settings = self.frozen, self.max_grad_norm
         finally:
             xb.set_step_source(None)
         self.step_no += 1
@@ -405,7 +406,9 @@ class Network:
     def replay(self, x, labels):
         """The next training step from the captured graph; returns the per-sample losses (a buffer that the next
         replay overwrites).  The requests of the batch may be other ones than at the capture (set_requests), not another number
-        of them, and the adapters have to be the captured ones (ValueError)."""
+        of them; the adapters, `frozen` and `max_grad_norm` have to be the captured ones (ValueError)."""
+        if self._graph_settings != (self.frozen, self.max_grad_norm):
+            raise ValueError("replay(): the step was captured with frozen = %r and max_grad_norm = %r; capture it again" % self._graph_settings)
         if [t.data_ptr() for t in self._adapter_tensors()] != [t.data_ptr() for t in self._graph_tensors]:
             raise ValueError("replay(): requests or adapters are no longer those that the captured step reads (switched on or off, another "
                              "number of rows, new or compacted adapters); capture the step again")

@@ -508,3 +508,15 @@ def test_replays_that_write_the_devices_leave_no_plane_valid(xb, no_graphs):
     ops.calls.clear()
     net.forward(x, 0)
     assert [c[0] for c in ops.calls].count("tile") == 2
+
+
+def test_replays_with_other_settings_are_refused(xb, no_graphs):
+    net, ops, x, labels = _adapted(xb)
+    net.capture(x, labels, 0.1)
+    for name, value in (("frozen", False), ("max_grad_norm", None), ("max_grad_norm", 1.0)):
+        kept = getattr(net, name)
+        setattr(net, name, value)
+        with pytest.raises(ValueError):
+            net.replay(x, labels)
+        setattr(net, name, kept)
+        net.replay(x, labels)
