@@ -330,6 +330,11 @@ class Network:
         for layer in self.layers:
             layer.programmed = None
 
+    def _keep_programmed(self):
+        if self.frozen:
+            for layer in self.layers:
+                layer.keep_programmed(self.step_no, self.ws)
+
     def add_adapters(self, count, rank, scale=1.0, seed=0):
         """`count` low-rank adapters beside every fully connected layer; which row of a batch uses which: set_requests."""
         for layer in self.layers:
@@ -378,13 +383,15 @@ class Network:
         noise comes from a counter in device memory that the graph itself advances.  Runs one real step (the
         warm-up of the capture) and returns its losses; every `replay(x, labels)` is the next step."""
         # The circuit-level model runs when step % fcm_every == 0, a test the host makes per step: a graph would
-        # freeze its outcome at capture time (a refresh on every replay, or on none).
-        if self.fcm_every > 1 and any(L.cfg.flags & xb.NI_WIRE_PROFILE for L in self.layers):
+        # freeze its outcome at capture time (a refresh on every replay, or on none).  A frozen network programs, and refreshes,
+        # outside the captured step.
+        if not self.frozen and self.fcm_every > 1 and any(L.cfg.flags & xb.NI_WIRE_PROFILE for L in self.layers):
             raise ValueError("capture(): the stored-profile wire model with fcm_every > 1 refreshes its profile on some "
                              "steps only, which a captured graph cannot express; run those steps eagerly")
         self._graph_x, self._graph_labels = x.clone(), labels.clone()
         self._graph_counter = torch.full((1,), self.step_no, dtype=torch.int64, device=x.device)
         main, side = torch.cuda.current_stream(), torch.cuda.Stream()
+        self._keep_programmed()
         side.wait_stream(main)
         xb.set_step_source(self._graph_counter)
         try:
@@ -412,11 +419,9 @@ class Network:
         if [t.data_ptr() for t in self._adapter_tensors()] != [t.data_ptr() for t in self._graph_tensors]:
             raise ValueError("replay(): requests or adapters are no longer those that the captured step reads (switched on or off, another "
                              "number of rows, new or compacted adapters); capture the step again")
-        if self.frozen:                    # the captured step reads the planes as they are
-            for layer in self.layers:
-                layer.keep_programmed(self.step_no, self.ws)
-        else:
-            self.reprogram()               # it writes the devices
+        self._keep_programmed()            # a captured step of a frozen network reads the planes as they are,
+        if not self.frozen:                # any other writes the devices
+            self.reprogram()
         self._graph_x.copy_(x)
         self._graph_labels.copy_(labels)
         self._graph.replay()

@@ -520,3 +520,34 @@ def test_replays_with_other_settings_are_refused(xb, no_graphs):
             net.replay(x, labels)
         setattr(net, name, kept)
         net.replay(x, labels)
+
+
+def test_frozen_network_with_a_stored_profile_is_captured(xb, no_graphs):
+    """It refreshes the profile only when it programs, which a captured step does not; the schedule is that of eager steps."""
+    import workloads
+    kw = workloads.config_kwargs("mlp")
+    flags = (kw["flags"] & ~workloads.NI_WIRE_AAM) | workloads.NI_WIRE_PROFILE
+
+    def steps(captured):
+        net, ops, x, labels = _adapted(xb)
+        for L in net.layers:
+            L.cfg.flags |= flags & workloads.NI_WIRE_PROFILE
+            L.cfg.flags &= ~workloads.NI_WIRE_AAM
+        net.ws = net.ws.new_empty(max(L.workspace_bytes(6) for L in net.layers))
+        net.fcm_every, net.step_no = 3, 3
+        net.frozen = False
+        net.train_step(x, labels, 0.1)
+        net.frozen = True
+        ops.calls.clear()
+        net.capture(x, labels, 0.1) if captured else net.train_step(x, labels, 0.1)          # step 4: no refresh
+        net.layers[0].W.mul_(0.5)
+        net.replay(x, labels) if captured else net.train_step(x, labels, 0.1)                # step 5: programmed again, no refresh
+        net.layers[0].W.mul_(0.5)
+        net.replay(x, labels) if captured else net.train_step(x, labels, 0.1)                # step 6: programmed again and refreshed
+        return [c[0] + str(c[1]["step"]) for c in ops.calls if c[0] in ("tile", "fcm_profile")], net, x, labels
+    assert steps(False)[0] == ["tile4", "tile4", "tile5", "fcm_profile6", "tile6"]
+    got, net, x, labels = steps(True)
+    assert got == ["tile4", "tile4", "tile5", "fcm_profile6", "tile6"]
+    net.frozen = False
+    with pytest.raises(ValueError):                               # steps that write the devices refresh on some of them only, as before
+        net.capture(x, labels, 0.1)
