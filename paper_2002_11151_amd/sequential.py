@@ -105,11 +105,11 @@ class Sequential(Network):
         return x
 
     def backward(self, d, step, lr):
-        first_layer = next(i for i, (kind, _) in enumerate(self.stack) if kind == "layer")
-        for i in range(len(self.stack) - 1, -1, -1):
+        first = next(i for i, (kind, _) in enumerate(self.stack) if kind in ("layer", "groupnorm"))      # that learns
+        for i in range(len(self.stack) - 1, first - 1, -1):
             kind, arg = self.stack[i]
             if kind == "layer":
-                d = arg.backward(d, step, lr, self.ws, need_dx=i != first_layer)
+                d = arg.backward(d, step, lr, self.ws, need_dx=i != first)
             elif kind == "relu":
                 d = self.ops.relu_bwd(self.saved[i], d)
             elif kind == "sigmoid":
@@ -120,5 +120,3 @@ class Sequential(Network):
                 d = self.ops.maxpool_bwd(d, self.saved[i], arg)
             else:
                 d = d.reshape(self.saved[i])
-            if d is None:
-                break

@@ -551,3 +551,21 @@ def test_frozen_network_with_a_stored_profile_is_captured(xb, no_graphs):
     net.frozen = False
     with pytest.raises(ValueError):                               # steps that write the devices refresh on some of them only, as before
         net.capture(x, labels, 0.1)
+
+
+@pytest.mark.parametrize("clipped", [False, True])
+def test_a_normalisation_before_the_first_weight_layer_learns(xb, clipped):
+    """Errors go back as far as something learns, no further."""
+    import torch
+    net, ops = _network(xb, [("flatten",), ("groupnorm", 3, "none"), ("flatten",), ("fc", 20), ("relu",), ("fc", 5)])
+    x, labels = _batch()
+    net.calibrate(x, labels)
+    net.max_grad_norm = 0.5 if clipped else None
+    norm = net.stack[1][1][0]
+    norm.gamma.copy_(torch.linspace(0.5, 1.5, 12))
+    before = norm.gamma.clone(), norm.beta.clone()
+    ops.calls.clear()
+    net.train_step(x, labels, 0.1)
+    names = [c[0] for c in ops.calls]
+    assert names == ["gn_fwd", "tile", "fwd", "tile", "fwd", "bwd", "update", "bwd", "update", "gn_bwd"] + (["clip_sgd"] if clipped else ["sgd"] * 2)
+    assert not torch.equal(norm.gamma, before[0]) and not torch.equal(norm.beta, before[1])

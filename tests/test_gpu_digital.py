@@ -565,3 +565,22 @@ def test_weights_loaded_into_a_frozen_network(xb):
         assert torch.equal(a.planes, b.planes)
         dy = torch.randn((3, a.N), device="cuda")
         assert torch.equal(xb.bwd(a.cfg, fresh, dy, a.K, a.w_max, 4.0), xb.bwd(a.cfg, a.planes, dy, a.K, a.w_max, 4.0))
+
+
+def test_normalisation_in_front_of_the_first_convolution(xb):
+    """Its parameters move by the gradients of the definition on the error that comes back through the convolution's crossbars."""
+    import workloads
+    from paper_2002_11151_amd import sequential
+    spec = [("groupnorm", 2, "silu"), ("conv", 8, 3, 1, 1), ("relu",), ("flatten",), ("fc", 10)]
+    net = sequential.Sequential(workloads.config_kwargs("resnet20"), spec, batch=5, in_shape=(7, 6, 4), seed=3)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(3)
+    x, labels = torch.randn((5, 7, 6, 4), generator=gen, device="cuda"), torch.arange(5, device="cuda").to(torch.int32)
+    net.calibrate(x, labels)
+    net.ops, norm = Recorder(xb), net.stack[0][1][0]
+    net.train_step(x, labels, 0.5)
+    (given, got), = [c[1:] for c in net.ops.calls if c[0] == "gn_bwd"]
+    _, dgamma, dbeta, _ = digital.gn_bwd(*(host(t) for t in given[:6]), "silu")
+    assert given[1].any()
+    for p, g, start in ((norm.gamma, dgamma, 1.0), (norm.beta, dbeta, 0.0)):
+        assert np.abs(host(p) - (start - 0.5 * g)).max() <= 1e-5 * np.abs(g).max() + 2 * U      # smooth activation: some 30 U of each term
