@@ -6,6 +6,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <climits>
 #include <cmath>
 #include <cstdint>
 
@@ -542,7 +543,7 @@ struct Plan {
     const int rows = (int)std::min<long long>(512, std::max<long long>(32, wanted));
     const int chunks = (positions + rows - 1) / rows;
     s = Shape{batch, positions, channels, groups, channels / groups, rows, chunks};
-    grid = dim3((unsigned)(batch * chunks), (unsigned)strips);
+    grid = dim3((unsigned)((long long)batch * chunks), (unsigned)strips);
     held_vec = s.per_group % 4 == 0 ? 4 : s.per_group % 2 == 0 ? 2 : 1;
     elements = (int)std::min<long long>(1 << 30, (long long)positions * (s.per_group / held_vec));
   }
@@ -568,9 +569,10 @@ struct Plan {
   size_t bytes() const { return align256(sums() * sizeof(double)) + align256((size_t)s.batch * s.groups * 2 * sizeof(double)); }
 };
 
-// The limits on a shape: elements below 2^38, threads of a launch below 2^32.
+// The limits on a shape: elements below 2^38, threads of a launch below 2^32, a block's positions and the 512 behind them within an int.
 int shape_ok(int batch, int positions, int channels, int groups) {
   if (batch <= 0 || positions <= 0 || channels <= 0 || groups <= 0 || channels % groups) return XBAR_ESHAPE;
+  if (positions > INT_MAX - 511) return XBAR_ESHAPE;
   if ((double)batch * positions * channels >= 274877906944.0 || channels > (1 << 20) || (double)batch * groups >= 33554432.0) return XBAR_ESHAPE;
   const Plan p(batch, positions, channels, groups);
   double threads = 256.0 * batch * p.s.chunks;

@@ -569,3 +569,29 @@ def test_a_normalisation_before_the_first_weight_layer_learns(xb, clipped):
     names = [c[0] for c in ops.calls]
     assert names == ["gn_fwd", "tile", "fwd", "tile", "fwd", "bwd", "update", "bwd", "update", "gn_bwd"] + (["clip_sgd"] if clipped else ["sgd"] * 2)
     assert not torch.equal(norm.gamma, before[0]) and not torch.equal(norm.beta, before[1])
+
+
+# ---- limits ----------------------------------------------------------------------------------------
+def test_group_norm_limits(xb):
+    """Both sides of every limit: 0 bytes and XBAR_ESHAPE beyond, a size and a refusal for the size alone (-4) inside."""
+    lib = xb.lib()
+    far = 1 << 45
+
+    def sizes(*shape):
+        nbytes = lib.xbar_gn_workspace_bytes(*shape)
+        assert nbytes < 1 << 44
+        codes = [lib.xbar_gn_fwd(P, P, P, None, far, P, P, *shape, 1e-5, 0, P, max(nbytes, 1) - 1, None),
+                 lib.xbar_gn_bwd(P, P, P, P, None, P, P, far, P, P, None, *shape, 0, P, max(nbytes, 1) - 1, None)]
+        assert codes == ([-4, -4] if nbytes else [-2, -2]), (shape, nbytes, codes)
+        return nbytes > 0
+    most = 2 ** 31 - 512
+    assert sizes(1, most, 1, 1) and not sizes(1, most + 1, 1, 1) and not sizes(1, 2 ** 31 - 1, 1, 1) and not sizes(1, 2 ** 31 - 1, 127, 1)
+    assert sizes(1, most, 127, 127) and not sizes(1, most, 129, 129)                           # 2^38 elements
+    assert sizes(4, most, 8, 1) and not sizes(5, most, 8, 1)                                   # batch ceil(positions / 512) below 2^24
+    assert sizes((1 << 23) - 8, 513, 8, 1) and not sizes((1 << 23) - 8, 1025, 8, 1)
+    assert sizes(1, 1, 1 << 20, 1) and not sizes(1, 1, (1 << 20) + 1, 1)
+    for values in (1, 64, 255, 256):                                                           # batch groups below 2^25 for short groups,
+        assert sizes((1 << 22) - 1, 1, 8 * values, 8) and not sizes(1 << 22, 1, 8 * values, 8)
+    for values in (257, 1024, 4096, 4100, 16384):                                              # up to 2^23 - 8 for all
+        assert sizes((1 << 20) - 1, 1, 8 * values, 8)
+    assert not sizes(1 << 20, 1, 8 * 16384, 8)

@@ -584,3 +584,34 @@ def test_normalisation_in_front_of_the_first_convolution(xb):
     assert given[1].any()
     for p, g, start in ((norm.gamma, dgamma, 1.0), (norm.beta, dbeta, 0.0)):
         assert np.abs(host(p) - (start - 0.5 * g)).max() <= 1e-5 * np.abs(g).max() + 2 * U      # smooth activation: some 30 U of each term
+
+
+def test_group_norm_of_the_most_positions(xb):
+    """2^31 - 512 positions of one channel: what lies at their end, the statistics, and (sums of blocks up to the last) dgamma and dbeta."""
+    n = 2 ** 31 - 512
+    x = torch.empty((1, n, 1), device="cuda").normal_()
+    one, half = torch.ones(1, device="cuda"), torch.full((1,), 0.5, device="cuda")
+    y, mean, invstd = xb.gn_fwd(x, one, half, 1)
+    total = [0.0, 0.0]
+    for part in x.reshape(-1).split(2 ** 28):
+        total = [total[0] + float(part.double().sum()), total[1] + float(part.double().square().sum())]
+    m = total[0] / n
+    within(mean, np.array([[m]]), 2 * U * abs(m) + 1e-12)
+    within(invstd, np.array([[(total[1] / n - m * m + 1e-5) ** -0.5]]), np.array([[2.2 * U]]))
+    m, i = host(mean)[0, 0], host(invstd)[0, 0]
+    want = lambda t: (host(t) - m) * i
+    for at in (slice(0, 1000), slice(n - 1000, n)):
+        z = want(x[0, at]) + 0.5
+        within(y[0, at], z, 1.01 * U * np.abs(z) + 1e-13)
+    del y
+    dy = torch.empty((1, n, 1), device="cuda").normal_()
+    dx, dgamma, dbeta = xb.gn_bwd(x, dy, one, half, mean, invstd)
+    s0 = s1 = size = 0.0
+    for g, part in zip(dy.reshape(-1).split(2 ** 28), x.reshape(-1).split(2 ** 28)):
+        g, xhat = g.double(), (part.double() - m) * i
+        s0, s1, size = s0 + float(g.sum()), s1 + float((g * xhat).sum()), size + float((g * xhat).abs().sum())
+    within(dbeta, np.array([s0]), np.array([1.01 * U * abs(s0) + 1e-12 * size]))
+    within(dgamma, np.array([s1]), np.array([1.01 * U * abs(s1) + 1e-12 * size]))
+    for at in (slice(0, 1000), slice(n - 1000, n)):
+        z = i * (host(dy[0, at]) - s0 / n - want(x[0, at]) * s1 / n)
+        within(dx[0, at], z, 1.01 * U * np.abs(z) + 1e-12)
