@@ -788,6 +788,22 @@ int with_kernels(int type, bool quads, int rank, F f) {
   return quads ? with_rank(float(), std::true_type()) : with_rank(float(), std::false_type());
 }
 
+struct Tensor {
+  const void* p;
+  size_t bytes;
+};
+// Whether something that is written lies over something that is read, or over the rest of it.
+template <size_t IN, size_t OUT>
+bool overlapping(const Tensor (&in)[IN], const Tensor (&out)[OUT]) {
+  for (size_t i = 0; i < OUT; ++i) {
+    for (const Tensor& q : in)
+      if (overlap(out[i].p, out[i].bytes, q.p, q.bytes)) return true;
+    for (size_t j = 0; j < i; ++j)
+      if (overlap(out[i].p, out[i].bytes, out[j].p, out[j].bytes)) return true;
+  }
+  return false;
+}
+
 }  // namespace
 
 extern "C" {
@@ -800,7 +816,9 @@ int xbar_adapter_plan(const int32_t* rows, int M, int adapters, void* plan, size
   if (shape_ok(M, 1, 1, 1, adapters)) return XBAR_ESHAPE;
   if (!aligned16(rows) || !aligned16(plan)) return XBAR_EALIGN;
   PlanAt p;
-  if (plan_bytes < plan_layout(plan, M, adapters, &p)) return XBAR_EWORKSPACE;
+  const size_t needed = plan_layout(plan, M, adapters, &p);
+  if (plan_bytes < needed) return XBAR_EWORKSPACE;
+  if (overlap(plan, needed, rows, (size_t)M * sizeof(int32_t))) return XBAR_EINVAL;
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   if (M <= kSmallPlan) {
     hipLaunchKernelGGL(plan_small_kernel, dim3(1), dim3(kSmallPlan), 0, st, rows, M, adapters, p);
@@ -832,11 +850,11 @@ int xbar_adapter_fwd(const void* plan, size_t plan_bytes, const float* base, con
   if (plan_bytes < plan_layout(const_cast<void*>(plan), M, adapters, &p)) return XBAR_EWORKSPACE;
   WorkAt w;
   if (ws_bytes < work_layout(ws, XBAR_OP_FWD, M, K, N, rank, adapters, &w)) return XBAR_EWORKSPACE;
-  const size_t x = (size_t)M * K * 4, y = (size_t)M * N * 4, t = (size_t)M * rank * 4, each = type == XBAR_BF16 ? 2 : 4;
-  const size_t a = (size_t)adapters * rank * K * each, b = (size_t)adapters * rank * N * each;
-  if ((Y != base && overlap(Y, y, base, y)) || overlap(Y, y, X, x) || overlap(Y, y, A, a) || overlap(Y, y, B, b) || overlap(Y, y, T, t) ||
-      overlap(T, t, X, x) || overlap(T, t, base, y) || overlap(T, t, A, a) || overlap(T, t, B, b))
-    return XBAR_EINVAL;
+  const size_t each = type == XBAR_BF16 ? 2 : 4, y = (size_t)M * N * 4;
+  const Tensor in[] = {{plan, plan_layout(nullptr, M, adapters, nullptr)}, {X, (size_t)M * K * 4}, {A, (size_t)adapters * rank * K * each},
+                       {B, (size_t)adapters * rank * N * each}, {scale, (size_t)adapters * 4}, {Y != base ? base : nullptr, y}};
+  const Tensor out[] = {{Y, y}, {T, (size_t)M * rank * 4}, {ws, work_layout(nullptr, XBAR_OP_FWD, M, K, N, rank, adapters, nullptr)}};
+  if (overlapping(in, out)) return XBAR_EINVAL;
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   const Split s(M, K, adapters);
   const int rc = with_kernels(type, K % 4 == 0, rank, [&](auto k) { return k.shrink(p, X, A, w.part, M, K, rank, adapters, s, st); });
@@ -859,16 +877,11 @@ int xbar_adapter_bwd(const void* plan, size_t plan_bytes, const float* base, con
   WorkAt w;
   if (ws_bytes < work_layout(ws, XBAR_OP_BWD, M, K, N, rank, adapters, &w)) return XBAR_EWORKSPACE;
   const size_t each = type == XBAR_BF16 ? 2 : 4, na = (size_t)adapters * rank * K, nb = (size_t)adapters * rank * N;
-  struct Tensor { const void* p; size_t bytes; };
-  const Tensor in[] = {{dY, (size_t)M * N * 4}, {X, (size_t)M * K * 4}, {T, (size_t)M * rank * 4}, {A, na * each}, {B, nb * each},
-                       {dX && dX != base ? base : nullptr, (size_t)M * K * 4}};
-  const Tensor out[] = {{dX, (size_t)M * K * 4}, {dA, na * 4}, {dB, nb * 4}};
-  for (int i = 0; i < 3; ++i) {
-    for (const Tensor& q : in)
-      if (overlap(out[i].p, out[i].bytes, q.p, q.bytes)) return XBAR_EINVAL;
-    for (int j = 0; j < i; ++j)
-      if (overlap(out[i].p, out[i].bytes, out[j].p, out[j].bytes)) return XBAR_EINVAL;
-  }
+  const Tensor in[] = {{plan, plan_layout(nullptr, M, adapters, nullptr)}, {dY, (size_t)M * N * 4}, {X, (size_t)M * K * 4}, {T, (size_t)M * rank * 4},
+                       {A, na * each}, {B, nb * each}, {scale, (size_t)adapters * 4}, {dX && dX != base ? base : nullptr, (size_t)M * K * 4}};
+  const Tensor out[] = {{dX, (size_t)M * K * 4}, {dA, na * 4}, {dB, nb * 4},
+                        {ws, work_layout(nullptr, XBAR_OP_BWD, M, K, N, rank, adapters, nullptr)}};
+  if (overlapping(in, out)) return XBAR_EINVAL;
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   const Split s(M, N, adapters);
   int rc = with_kernels(type, N % 4 == 0, rank, [&](auto k) { return k.shrink(p, dY, B, w.part, M, N, rank, adapters, s, st); });

@@ -595,3 +595,33 @@ def test_group_norm_limits(xb):
     for values in (257, 1024, 4096, 4100, 16384):                                              # up to 2^23 - 8 for all
         assert sizes((1 << 20) - 1, 1, 8 * values, 8)
     assert not sizes(1 << 20, 1, 8 * 16384, 8)
+
+
+def test_adapter_outputs_over_plans_scales_and_workspaces_are_refused(xb):
+    """An output over an input, the plan, another output or the workspace, or a workspace or plan over an input, by its first or last bytes."""
+    lib = xb.lib()
+    M, K, N, rank, n = 8, 16, 24, 4, 3
+    plan, fwd_ws, bwd_ws = lib.xbar_adapter_plan_bytes(M, n), *(lib.xbar_adapter_workspace_bytes(op, M, K, N, rank, n) for op in (xb.OP_FWD, xb.OP_BWD))
+    at = {name: (i + 1) << 32 for i, name in enumerate("plan base X A B scale Y T ws dY dX dA dB".split())}
+    fwd = lambda **kw: (lambda a: lib.xbar_adapter_fwd(a["plan"], plan, a["base"], a["X"], a["A"], a["B"], 0, a["scale"], a["Y"], a["T"], M, K, N, rank, n,
+                                                       a["ws"], fwd_ws, None))(dict(at, **kw))
+    bwd = lambda **kw: (lambda a: lib.xbar_adapter_bwd(a["plan"], plan, a["base"], a["dY"], a["X"], a["T"], a["A"], a["B"], 0, a["scale"], a["dX"], a["dA"],
+                                                       a["dB"], M, K, N, rank, n, a["ws"], bwd_ws, None))(dict(at, **kw))
+    bytes_of = dict(plan=plan, base=4 * M * N, X=4 * M * K, A=4 * n * rank * K, B=4 * n * rank * N, scale=4 * n, Y=4 * M * N, T=4 * M * rank, dY=4 * M * N,
+                    dX=4 * M * K, dA=4 * n * rank * K, dB=4 * n * rank * N)
+    last = lambda name: at[name] + (bytes_of[name] - 1) // 16 * 16
+    for out, others in (("Y", "X A B scale plan T"), ("T", "X A B scale plan base Y")):
+        for other in others.split():
+            assert fwd(**{out: at[other]}) == fwd(**{out: last(other)}) == -1, (out, other)
+        assert fwd(**{out: at["ws"]}) == fwd(**{out: at["ws"] + fwd_ws - 16}) == -1
+    for out in ("dX", "dA", "dB"):
+        for other in "dY X T A B scale plan dX dA dB".split():
+            if other != out:
+                assert bwd(**{out: at[other]}) == bwd(**{out: last(other)}) == -1, (out, other)
+        assert bwd(**{out: at["ws"]}) == bwd(**{out: at["ws"] + bwd_ws - 16}) == -1
+    for call, size, others in ((fwd, fwd_ws, "base X A B scale plan"), (bwd, bwd_ws, "base dY X T A B scale plan")):
+        bytes_of["base"] = 4 * M * (N if call is fwd else K)
+        for other in others.split():
+            assert call(ws=last(other)) == call(ws=at[other] - (size - 1) // 16 * 16) == -1, other
+    assert fwd(ws=at["base"], Y=at["base"]) == bwd(ws=at["base"], dX=at["base"]) == -1
+    assert lib.xbar_adapter_plan(at["X"], M, n, at["X"] + 16, plan, None) == lib.xbar_adapter_plan(at["X"], M, n, at["X"] - plan + 16, plan, None) == -1
