@@ -385,7 +385,7 @@ int xbar_absmax(const float* x, size_t n, float* result, void* ws, size_t ws_byt
  *            forward pass had); dx, dgamma = sum g xhat, dbeta = sum g over batch and positions, dskip = g (NULL: not wanted; only
  *            with skip)
  *   act      XBAR_ACT_*; a ReLU's output and gradient are 0 where z is not above 0 (NaN too), as in relu_fwd
- * skip (shape of x) may be NULL.  Outputs must not overlap inputs (XBAR_EINVAL for y, dx and dskip).  Statistics are accumulated in
+ * skip (shape of x) may be NULL.  Outputs must not overlap inputs, ws or one another (XBAR_EINVAL for y, dx and dskip).  Statistics are accumulated in
  * double precision in a fixed order.  ws: xbar_gn_workspace_bytes, 0 where a shape is refused (XBAR_ESHAPE).  Accepted are channels
  * <= 2^20, positions <= 2^31 - 512, batch positions channels < 2^38, batch ceil(positions / 512) < 2^24 and batch groups <= 2^23 - 8, or
  * < 2^25 for groups of up to 256 values (some between the two as well).

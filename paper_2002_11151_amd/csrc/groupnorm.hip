@@ -681,8 +681,11 @@ int xbar_gn_fwd(const float* x, const float* gamma, const float* beta, const flo
     return XBAR_EALIGN;
   if (!(eps >= 0.0f) || !std::isfinite(eps) || act < XBAR_ACT_NONE || act > XBAR_ACT_SILU) return XBAR_EINVAL;
   const size_t n = (size_t)batch * positions * channels * sizeof(float);
-  if (overlap(y, n, x, n) || overlap(y, n, skip, n)) return XBAR_EINVAL;
+  const size_t each = (size_t)channels * sizeof(float), stats = (size_t)batch * groups * sizeof(float);
   const Plan p(batch, positions, channels, groups);
+  if (overlap(y, n, x, n) || overlap(y, n, skip, n) || overlap(y, n, gamma, each) || overlap(y, n, beta, each) || overlap(y, n, mean, stats) ||
+      overlap(y, n, invstd, stats) || overlap(y, n, ws, p.bytes()))
+    return XBAR_EINVAL;
   if (ws_bytes < p.bytes()) return XBAR_EWORKSPACE;
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   double* part = reinterpret_cast<double*>(ws);
@@ -705,10 +708,14 @@ int xbar_gn_bwd(const float* x, const float* dy, const float* gamma, const float
     return XBAR_EALIGN;
   if (act < XBAR_ACT_NONE || act > XBAR_ACT_SILU || (dskip && !skip)) return XBAR_EINVAL;
   const size_t n = (size_t)batch * positions * channels * sizeof(float);
-  if (overlap(dx, n, x, n) || overlap(dx, n, dy, n) || overlap(dx, n, skip, n) || overlap(dskip, n, x, n) || overlap(dskip, n, dy, n) ||
-      overlap(dskip, n, skip, n) || overlap(dskip, n, dx, n))
-    return XBAR_EINVAL;
+  const size_t each = (size_t)channels * sizeof(float), stats = (size_t)batch * groups * sizeof(float);
   const Plan p(batch, positions, channels, groups);
+  for (const float* out : {dx, dskip})
+    if (overlap(out, n, x, n) || overlap(out, n, dy, n) || overlap(out, n, skip, n) || overlap(out, n, gamma, each) || overlap(out, n, beta, each) ||
+        overlap(out, n, mean, stats) || overlap(out, n, invstd, stats) || overlap(out, n, dgamma, each) || overlap(out, n, dbeta, each) ||
+        overlap(out, n, ws, p.bytes()))
+      return XBAR_EINVAL;
+  if (overlap(dskip, n, dx, n)) return XBAR_EINVAL;
   if (ws_bytes < p.bytes()) return XBAR_EWORKSPACE;
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   double* part = reinterpret_cast<double*>(ws);

@@ -625,3 +625,22 @@ def test_adapter_outputs_over_plans_scales_and_workspaces_are_refused(xb):
             assert call(ws=last(other)) == call(ws=at[other] - (size - 1) // 16 * 16) == -1, other
     assert fwd(ws=at["base"], Y=at["base"]) == bwd(ws=at["base"], dX=at["base"]) == -1
     assert lib.xbar_adapter_plan(at["X"], M, n, at["X"] + 16, plan, None) == lib.xbar_adapter_plan(at["X"], M, n, at["X"] - plan + 16, plan, None) == -1
+
+
+def test_group_norm_outputs_over_parameters_statistics_and_workspaces_are_refused(xb):
+    lib = xb.lib()
+    at = {name: (i + 1) << 32 for i, name in enumerate("x dy gamma beta skip mean invstd y dgamma dbeta dskip dx ws".split())}
+    bytes_of = dict(gamma=48, beta=48, mean=24, invstd=24, dgamma=48, dbeta=48)
+    last = lambda name: at[name] + (bytes_of[name] - 1) // 16 * 16
+    ws = lib.xbar_gn_workspace_bytes(2, 9, 12, 3)
+    gn_fwd = lambda **kw: (lambda a: lib.xbar_gn_fwd(a["x"], a["gamma"], a["beta"], a["skip"], a["y"], a["mean"], a["invstd"], 2, 9, 12, 3, 1e-5, 0, a["ws"], ws,
+                                                     None))(dict(at, **kw))
+    gn_bwd = lambda **kw: (lambda a: lib.xbar_gn_bwd(a["x"], a["dy"], a["gamma"], a["beta"], a["skip"], a["mean"], a["invstd"], a["dx"], a["dgamma"], a["dbeta"],
+                                                     a["dskip"], 2, 9, 12, 3, 0, a["ws"], ws, None))(dict(at, **kw))
+    for other in "gamma beta mean invstd".split():
+        assert gn_fwd(y=at[other]) == gn_fwd(y=last(other)) == -1, other
+    assert gn_fwd(y=at["ws"]) == gn_fwd(y=at["ws"] + ws - 16) == -1
+    for out in ("dx", "dskip"):
+        for other in "gamma beta mean invstd dgamma dbeta".split():
+            assert gn_bwd(**{out: at[other]}) == gn_bwd(**{out: last(other)}) == -1, (out, other)
+        assert gn_bwd(**{out: at["ws"]}) == gn_bwd(**{out: at["ws"] + ws - 16}) == -1
