@@ -413,9 +413,9 @@ int xbar_gn_bwd(const float* x, const float* dy, const float* gamma, const float
  *                 not wanted, base is not read); dA[a][r][k] = sum_m dT[m][r] X[m][k], dB[a][r][n] = scale[a] sum_m T[m][r] dY[m][n] over the rows
  *                 of adapter a (zero where it has none), float whatever the adapters' type
  * Products and sums in single precision, in a fixed order.  What is written (outputs, ws, a plan) must not overlap itself or, but for
- * the base, anything that is read: XBAR_EINVAL.  A plan made for another
- * M or number of adapters: nothing is written.  rank <= 128, adapters <= 65536, M <= 2^24, rank K and rank N < 2^30, M max(K, N) < 2^38, (M / 32 + adapters) (K + N) / 64 < 2^24,
- * else XBAR_ESHAPE.
+ * the base, anything that is read: XBAR_EINVAL.  A plan made for another M or number of adapters: nothing is written.
+ * Accepted are rank <= 128, adapters <= 65536, M <= 2^24, K and N < 2^24, rank max(K, N) < 2^30 and
+ * (M / 32 + adapters + 8) (K + N + 126) / 64 < 2^24 (some shapes beyond the last as well); XBAR_ESHAPE where xbar_adapter_workspace_bytes is 0.
  * ws: xbar_adapter_workspace_bytes(XBAR_OP_FWD or XBAR_OP_BWD, ...).
  */
 #define XBAR_F32  0

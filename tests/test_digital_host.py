@@ -644,3 +644,18 @@ def test_group_norm_outputs_over_parameters_statistics_and_workspaces_are_refuse
         for other in "gamma beta mean invstd dgamma dbeta".split():
             assert gn_bwd(**{out: at[other]}) == gn_bwd(**{out: last(other)}) == -1, (out, other)
         assert gn_bwd(**{out: at["ws"]}) == gn_bwd(**{out: at["ws"] + ws - 16}) == -1
+
+
+def test_adapter_limits(xb):
+    """Shapes just inside the stated limits have a workspace, those beyond the exact ones do not."""
+    size = lambda M=8, K=16, N=24, rank=4, n=3: xb.lib().xbar_adapter_workspace_bytes(xb.OP_FWD, M, K, N, rank, n) > 0
+    top = (1 << 24) - 1
+    assert size(M=1 << 24, K=1, N=1, n=65536) and not size(M=(1 << 24) + 1, K=1, N=1)
+    assert size(K=top, rank=1) and not size(K=1 << 24, rank=1) and size(N=top, rank=1) and not size(N=1 << 24, rank=1)
+    assert size(K=top, rank=64, n=1) and not size(K=top, rank=65, n=1)                         # rank max(K, N) below 2^30
+    assert size(M=1, K=(1 << 17) - 1, N=1, rank=32, n=65536) and not size(M=1, K=1 << 17, N=1, rank=32, n=65536)    # adapters rank max(K, N) below 2^38
+    cost = lambda M, K, N, n: (M / 32 + n + 8) * (K + N + 126) / 64
+    for M, K, N, n in ((1 << 18, 8000, 2000, 65536), (1 << 24, 1000, 690, 65536), (28, 13_000_000, 13_000_000, 28), (65537, 7850, 7850, 65536),
+                       (1, 29, 1, 1), (300, 5000, 11000, 60000), (16, 16_000_000, 16_000_000, 16)):
+        assert cost(M, K, N, n) < 1 << 24 and size(M, K, N, 1, n), (M, K, N, n)
+    assert not size(M=65536, K=10000, N=10000, rank=1, n=65536) and not size(M=40, K=top, N=top, rank=1, n=40)
