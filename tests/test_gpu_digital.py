@@ -615,3 +615,93 @@ def test_group_norm_of_the_most_positions(xb):
     for at in (slice(0, 1000), slice(n - 1000, n)):
         z = i * (host(dy[0, at]) - s0 / n - want(x[0, at]) * s1 / n)
         within(dx[0, at], z, 1.01 * U * np.abs(z) + 1e-12)
+
+
+# ---- plans of many adapters; gradients beyond 32 bits ----------------------------------------------
+@pytest.mark.parametrize("M,n", [(200, 257), (256, 1100), (1, 65536), (257, 1023), (257, 1024), (600, 1025), (3000, 1500), (5000, 4100), (2500, 65536)])
+def test_adapters_with_plans_of_many(xb, M, n):
+    """Prefix sums over several thousand adapters, most of them without rows; batches of one launch with more adapters than threads."""
+    rows = mixed(M, n, M + n)
+    rows[0], rows[-1] = n - 1, 0
+    adapter_check(xb, adapter_case(rows, 5, 6, 2, n, M))
+
+
+def sums_of(t, *more, axes, step):
+    """Sums over `axes` of a product of device tensors in float64, `step` of the longest axis at a time (all of them broadcast along it)."""
+    at = int(np.argmax(t.shape))
+    total = 0.0
+    for part in zip(*[u.split(step, at) if u.shape[at] == t.shape[at] else [u] * -(-t.shape[at] // step) for u in (t, *more)]):
+        product = part[0].double()
+        for u in part[1:]:
+            product = product * u.double()
+        total = total + product.sum(axes)
+    return total
+
+
+@pytest.mark.parametrize("shape,groups", [((3, 12_000_000, 64), 4), ((2_200_000, 1, 1024), 4)], ids=["three_launches", "in_registers"])
+def test_group_norm_gradients_beyond_32_bits(xb, shape, groups):
+    """More than 2^31 elements, errors that have nothing to do with x: dx at both ends, all of dgamma and dbeta."""
+    B, C = shape[0], shape[-1]
+    gamma, beta = torch.linspace(0.5, 1.5, C, device="cuda"), torch.zeros(C, device="cuda")
+    x, dy = torch.empty(shape, device="cuda").normal_(), torch.empty(shape, device="cuda").normal_()
+    assert x.numel() > 2 ** 31
+    _, mean, invstd = xb.gn_fwd(x, gamma, beta, groups)
+    dx, dgamma, dbeta = xb.gn_bwd(x, dy, gamma, beta, mean, invstd)
+    of = lambda t: t.double().repeat_interleave(C // groups, dim=1)[:, None, :]           # [batch][groups] to [batch][1][channels]
+    m, i, step = of(mean), of(invstd), 400_000 if B == 3 else 60_000
+    s0 = sums_of(dy, axes=(0, 1), step=step)
+    s1 = sums_of(dy, x, i, axes=(0, 1), step=step) - sums_of(dy, m, i, axes=(0, 1), step=step)
+    size = x.numel() / C * 4.0                                                            # of the terms: normal numbers
+    within(dbeta, s0.cpu().numpy(), 1.01 * U * np.abs(s0.cpu().numpy()) + 1e-12 * size)
+    within(dgamma, s1.cpu().numpy(), 1.01 * U * np.abs(s1.cpu().numpy()) + 1e-12 * size)
+    for b in (0, B - 1):
+        g, xhat = gamma.double(), lambda t: (t.double() - m[b]) * i[b]
+        a0 = a1 = 0.0
+        for d, t in zip(dy[b].split(1_000_000), x[b].split(1_000_000)):
+            a0, a1 = a0 + (g * d.double()).sum(0), a1 + (g * d.double() * xhat(t)).sum(0)
+        mean_of = lambda a: (a.reshape(groups, -1).sum(1) / (shape[1] * C // groups)).repeat_interleave(C // groups)
+        for part in (slice(0, 500), slice(-500, None)):
+            want = i[b] * (g * dy[b, part].double() - mean_of(a0) - xhat(x[b, part]) * mean_of(a1))
+            want = want.cpu().numpy()
+            within(dx[b, part], want, 1.01 * U * np.abs(want) + 1e-11)
+
+
+def test_adapter_gradients_beyond_32_bits(xb):
+    """Adapters, gradients and partial gradients of more than 2^31 elements each: the last columns of adapters with one chunk of rows and with several,
+    at both ends; T and dX of the last rows."""
+    M, K, N, rank, n = 8192, 600_000, 8, 128, 40
+    at = torch.arange(M, device="cuda")
+    rows = torch.where(at % 6 < 5, at % 6, 5 + (at // 6) % (n - 5)).to(torch.int32)
+    rows[-1] = n - 1
+    counts = torch.bincount(rows.long(), minlength=n).tolist()
+    slots = sum(-(-c // 256) for c in counts if c > 256)                                  # chunks of 256 rows
+    assert n * rank * K > 2 ** 31 and slots * rank * K > 2 ** 31 and min(counts) > 0 and counts[n - 1] <= 256 < counts[4]
+    X, A = torch.empty((M, K), device="cuda").normal_(), torch.empty((n, rank, K), device="cuda").normal_()
+    B, scale = torch.randn((n, rank, N), device="cuda"), 0.5 + torch.rand(n, device="cuda")
+    base, dY, back = torch.randn((M, N), device="cuda"), torch.randn((M, N), device="cuda"), X.clone()
+    plan = xb.adapter_plan(rows, n)
+    Y, T = xb.adapter_fwd(plan, base, X, A, B, scale)
+    dX, dA, dB = xb.adapter_bwd(plan, back, dY, X, T, A, B, scale, out=back)
+    chain = lambda k: (k / 4 + 48) * U
+    for m in (M - 1, M - 2):
+        a = int(rows[m])
+        x, w = X[m].double(), A[a].double()
+        within(T[m], torch.mv(w, x).cpu().numpy(), chain(K) * torch.mv(w.abs(), x.abs()).cpu().numpy())
+        t = T[m].double() * scale[a].double()
+        want, size = torch.mv(B[a].double().t().contiguous(), t), torch.mv(B[a].double().abs().t().contiguous(), t.abs())
+        within(Y[m], (base[m].double() + want).cpu().numpy(), ((chain(rank) + 4 * U) * size + 2 * U * (size + base[m].abs())).cpu().numpy())
+        dT = torch.mv(B[a].double(), dY[m].double()) * scale[a].double()
+        aT = torch.mv(B[a].double().abs(), dY[m].double().abs()) * scale[a].double()
+        want, size = x + torch.mv(w.t().contiguous(), dT), torch.mv(w.abs().t().contiguous(), aT)
+        within(dX[m], want.cpu().numpy(), ((chain(N) + chain(rank) + 4 * U) * size + 2 * U * (x.abs() + want.abs())).cpu().numpy())
+    for a in (0, 4, 5, n - 1):
+        mine = (rows == a).nonzero().flatten()
+        y, f = dY[mine].double(), scale[a].double()
+        dT, aT = (torch.matmul(u, v.t().contiguous()) * f for u, v in ((y, B[a].double()), (y.abs(), B[a].double().abs())))
+        for cols in (slice(0, 64), slice(K - 64, K)):
+            x = X[mine, cols].double()
+            want, size = torch.matmul(dT.t().contiguous(), x), torch.matmul(aT.t().contiguous(), x.abs())
+            within(dA[a][:, cols], want.cpu().numpy(), (chain(N) + chain(M) + 4 * U) * size.cpu().numpy())
+        t = T[mine].double()
+        want, size = (torch.matmul(u.t().contiguous(), v) * f for u, v in ((t, y), (t.abs(), y.abs())))
+        within(dB[a], want.cpu().numpy(), (chain(M) + 4 * U) * size.cpu().numpy())
