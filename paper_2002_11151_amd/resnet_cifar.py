@@ -358,12 +358,10 @@ class Network:
         self.requests = self._plan = self.ops.adapter_plan(rows, self.adapter_count)
 
     def _adapter_tensors(self):
-        """What kernels of this batch know of the adapters, by address: the plan, every layer's parameters.  (Tensors of their own on
-        the same memory, which stays as long as they do.)"""
+        """What kernels of this batch know of the adapters, by address: the plan, every layer's parameters."""
         if self.requests is None:
-            return ()
-        own = [t for L in self.layers if L.adapters is not None for t in (L.adapters.A, L.adapters.B, L.adapters.scale)]
-        return tuple(t.detach() for t in (self.requests.buffer, *own))
+            return []
+        return [self.requests.buffer] + [t for L in self.layers if L.adapters is not None for t in (L.adapters.A, L.adapters.B, L.adapters.scale)]
 
     def train_step(self, x, labels, lr):
         """One SGD step on a batch: returns the per-sample losses (device tensor)."""
@@ -403,7 +401,8 @@ class Network:
             with torch.cuda.graph(self._graph, stream=side):
                 self._graph_loss = self._counted_step(lr)
             self.grad_norm, self._graph_norm = norm, self.grad_norm        # the graph's own: not computed before the first replay
-            self._graph_plan, self._graph_tensors = self.requests, self._adapter_tensors()
+            # (tensors of their own on that memory: it stays, whatever becomes of the layers' tensors)
+            self._graph_plan, self._graph_tensors = self.requests, [t.detach() for t in self._adapter_tensors()]
             self._graph_settings = self.frozen, self.max_grad_norm
         finally:
             xb.set_step_source(None)

@@ -705,3 +705,34 @@ def test_adapter_gradients_beyond_32_bits(xb):
         t = T[mine].double()
         want, size = (torch.matmul(u.t().contiguous(), v) * f for u, v in ((t, y), (t.abs(), y.abs())))
         within(dB[a], want.cpu().numpy(), (chain(M) + 4 * U) * size.cpu().numpy())
+
+
+@pytest.mark.parametrize("frozen", [False, True])
+def test_captured_steps_with_batch_norm_and_changing_requests(xb, frozen):
+    """A residual network whose batch norms and adapters step together, clipped, its devices written or not: replays are the eager steps."""
+    import workloads
+    from paper_2002_11151_amd import resnet_cifar
+
+    def make():
+        net = resnet_cifar.ResNetCifar(workloads.config_kwargs("resnet20"), batch=4, n_blocks=1, image=8, classes=10, widths=(16, 32, 64), seed=4)
+        gen = torch.Generator(device="cuda")
+        gen.manual_seed(6)
+        x, labels = torch.randn((4, 8, 8, 3), generator=gen, device="cuda"), torch.arange(4, device="cuda").to(torch.int32)
+        net.calibrate(x, labels)
+        net.frozen, net.max_grad_norm = frozen, 0.5
+        net.add_adapters(3, 5)
+        return net, x, labels
+    (eager, x, labels), (graphed, _, _) = make(), make()
+    turns = [dev(t, np.int32) for t in ([1, 0, -1, 2], [2, 2, 2, 2], [-1, -1, -1, -1], [0, 1, 2, 0])]
+    want, got = [], []
+    for k, rows in enumerate(turns):
+        for net, out in ((eager, want), (graphed, got)):
+            net.set_requests(rows)
+            step = net.train_step if net is eager else net.replay if k else net.capture
+            out.append((step(x, labels).clone() if step == net.replay else step(x, labels, 0.02).clone(), net.grad_norm.clone()))
+            torch.cuda.synchronize()
+    assert all(torch.equal(a, b) and torch.equal(c, d) for (a, c), (b, d) in zip(got, want))
+    for a, b in zip(eager.layers, graphed.layers):
+        assert torch.equal(a.W, b.W)
+    a, b = eager.fc.adapters, graphed.fc.adapters
+    assert torch.equal(a.A, b.A) and torch.equal(a.B, b.B) and b.B.any() and torch.equal(eager.stem_bn.gamma, graphed.stem_bn.gamma)
