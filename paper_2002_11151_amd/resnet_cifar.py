@@ -407,6 +407,7 @@ class Network:
         finally:
             xb.set_step_source(None)
         self.step_no += 1
+        self._graph_step = self.step_no
         return first
 
     def replay(self, x, labels):
@@ -423,9 +424,12 @@ class Network:
             self.reprogram()
         self._graph_x.copy_(x)
         self._graph_labels.copy_(labels)
+        if self._graph_step != self.step_no:      # eager steps, which do not advance the captured step's counter, ran since
+            self._graph_counter.fill_(self.step_no)
         self._graph.replay()
         self.grad_norm = self._graph_norm
         self.step_no += 1
+        self._graph_step = self.step_no
         return self._graph_loss
 
     def _counted_step(self, lr):

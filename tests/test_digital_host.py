@@ -659,3 +659,12 @@ def test_adapter_limits(xb):
                        (1, 29, 1, 1), (300, 5000, 11000, 60000), (16, 16_000_000, 16_000_000, 16)):
         assert cost(M, K, N, n) < 1 << 24 and size(M, K, N, 1, n), (M, K, N, n)
     assert not size(M=65536, K=10000, N=10000, rank=1, n=65536) and not size(M=40, K=top, N=top, rank=1, n=40)
+
+
+def test_replays_count_the_eager_steps_between_them(xb, no_graphs):
+    net, ops, x, labels = _adapted(xb)
+    net.capture(x, labels, 0.1)
+    net.train_step(x, labels, 0.1)
+    net.train_step(x, labels, 0.1)
+    net.replay(x, labels)                                         # (it advances nothing here)
+    assert int(net._graph_counter) == 3 and net.step_no == 4

@@ -736,3 +736,16 @@ def test_captured_steps_with_batch_norm_and_changing_requests(xb, frozen):
         assert torch.equal(a.W, b.W)
     a, b = eager.fc.adapters, graphed.fc.adapters
     assert torch.equal(a.A, b.A) and torch.equal(a.B, b.B) and b.B.any() and torch.equal(eager.stem_bn.gamma, graphed.stem_bn.gamma)
+
+
+def test_eager_steps_between_replays(xb):
+    """The captured step keys its write noise by the step that it is, whatever steps ran before it."""
+    (eager, x, labels), (mixed_, _, _) = perceptron(xb), perceptron(xb)
+    assert all(L.cfg.flags & xb.NI_UPD_NOISE and L.cfg.upd_noise_gamma > 0 for L in eager.layers)
+    eager.frozen = mixed_.frozen = False
+    want = [eager.train_step(x, labels, 0.1).clone() for _ in range(5)]
+    got = [mixed_.capture(x, labels, 0.1).clone(), mixed_.train_step(x, labels, 0.1).clone()]
+    got += [mixed_.replay(x, labels).clone(), mixed_.train_step(x, labels, 0.1).clone(), mixed_.replay(x, labels).clone()]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert all(torch.equal(a.W, b.W) for a, b in zip(eager.layers, mixed_.layers))
