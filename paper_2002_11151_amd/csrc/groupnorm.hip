@@ -442,45 +442,45 @@ __global__ __launch_bounds__(256) void gn_partial_kernel(const float* x, const f
   }
 }
 
-// One wave per sample and group: forward mean and 1 / std, backward the two means over the group that dx needs.
-template <bool BWD>
-__device__ __forceinline__ void group_of_wave(const double* part, const Shape& s, int item, const float* x, const float* gamma, float eps,
-                                              float* mean, float* invstd, double* coef) {
-  const int lane = threadIdx.x & 63, b = item / s.groups, g = item - b * s.groups;
-  const int values = s.chunks * s.per_group;
+// TEAM threads per sample and group: forward mean and 1 / std, backward the two means over the group that dx needs.  Eight loads of a thread
+// in flight.
+template <bool BWD, int TEAM>
+__global__ __launch_bounds__(team_block(TEAM)) void gn_final_kernel(const double* part, Shape s, const float* x, const float* gamma, float eps,
+                                                                    float* mean, float* invstd, double* coef) {
+  __shared__ double red[2][team_block(TEAM) / 64];
+  const int item = blockIdx.x * (team_block(TEAM) / TEAM) + threadIdx.x / TEAM, t = threadIdx.x % TEAM;
+  if (item >= s.batch * s.groups) return;                      // (all threads of a team, and a block is one team where it has to wait)
+  const int b = item / s.groups, g = item - b * s.groups, c0 = g * s.per_group, values = s.chunks * s.per_group;
+  const double* from = part + ((size_t)b * s.chunks * s.channels + c0) * 2;
   double s0 = 0.0, s1 = 0.0;
-  for (int i = lane; i < values; i += 64) {
-    const int chunk = i / s.per_group, c = g * s.per_group + (i - chunk * s.per_group);
-    const double* p = part + (((size_t)b * s.chunks + chunk) * s.channels + c) * 2;
-    const double f = BWD ? (double)gamma[c] : 1.0;
-    s0 = __builtin_fma(f, p[0], s0);
-    s1 = __builtin_fma(f, p[1], s1);
-  }
+  Walk at(t, TEAM, s.per_group);
+  for (int i0 = t; i0 < values; i0 += 8 * TEAM) {
+    double2 p[8];
+    float f[8];
 #pragma unroll
-  for (int d = 32; d; d >>= 1) {
-    s0 += __shfl_xor(s0, d, 64);
-    s1 += __shfl_xor(s1, d, 64);
+    for (int u = 0; u < 8; ++u, at.next())
+      if (i0 + u * TEAM < values) {
+        p[u] = *reinterpret_cast<const double2*>(from + ((size_t)at.row * s.channels + at.c) * 2);
+        if (BWD) f[u] = gamma[c0 + at.c];
+      }
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (i0 + u * TEAM < values) {
+        s0 = __builtin_fma(BWD ? (double)f[u] : 1.0, p[u].x, s0);
+        s1 = __builtin_fma(BWD ? (double)f[u] : 1.0, p[u].y, s1);
+      }
   }
-  if (lane) return;
+  team_sum<TEAM>(s0, s1, red);
+  if (t) return;
   const double n = (double)s.positions * s.per_group;
   if (BWD) {
     coef[(size_t)item * 2] = s0 / n;
     coef[(size_t)item * 2 + 1] = s1 / n;
   } else {
     const double m = s0 / n, var = s1 / n - m * m;
-    mean[item] = (float)((double)x[(size_t)b * s.positions * s.channels + g * s.per_group] + m);
+    mean[item] = (float)((double)x[(size_t)b * s.positions * s.channels + c0] + m);
     invstd[item] = (float)(1.0 / ::sqrt((var < 0.0 ? 0.0 : var) + (double)eps));
   }
-}
-
-__global__ __launch_bounds__(256) void gn_final_fwd_kernel(const double* part, Shape s, const float* x, float eps, float* mean, float* invstd) {
-  const int item = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (item < s.batch * s.groups) group_of_wave<false>(part, s, item, x, nullptr, eps, mean, invstd, nullptr);
-}
-
-__global__ __launch_bounds__(256) void gn_final_bwd_kernel(const double* part, Shape s, const float* gamma, double* coef) {
-  const int item = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (item < s.batch * s.groups) group_of_wave<true>(part, s, item, nullptr, gamma, 0.0f, nullptr, nullptr, coef);
 }
 
 // y, or dx and dskip; blocks and threads as in gn_partial_kernel.  PAST: outputs of more than half of the last-level cache, which the next
@@ -564,6 +564,16 @@ struct Plan {
     const int teams = team_block(team) / team;
     const long long blocks = ((long long)s.batch * s.groups + teams - 1) / teams;
     return dim3((unsigned)((blocks + kXcds - 1) / kXcds * kXcds));
+  }
+  // A block of 1024 threads per group where there are few groups of many pairs of sums, else a wave (us, block / wave: one group of 25088 pairs 6.8 / 37,
+  // of 564 3.0 / 2.5; 256 groups of 1600 4.8 / 6.4, of 512 4.9 / 4.9; 512 of 1600 6.2 / 6.7; 2048 of 800 15.7 / 7.3).
+  template <bool BWD>
+  void finish(const double* part, const float* x, const float* gamma, float eps, float* mean, float* invstd, double* coef, hipStream_t st) const {
+    const int items = s.batch * s.groups;
+    const bool block = items <= 512 && (long long)s.chunks * s.per_group > 1024;
+    auto k = block ? gn_final_kernel<BWD, 1024> : gn_final_kernel<BWD, 64>;
+    hipLaunchKernelGGL(k, dim3((unsigned)(block ? items : (items + 3) / 4)), dim3(block ? 1024 : 256), 0, st, part, s, x, gamma, eps, mean, invstd,
+                       coef);
   }
   size_t sums() const { return (size_t)s.batch * s.chunks * s.channels * 2; }
   size_t bytes() const { return align256(sums() * sizeof(double)) + align256((size_t)s.batch * s.groups * 2 * sizeof(double)); }
@@ -693,7 +703,7 @@ int xbar_gn_fwd(const float* x, const float* gamma, const float* beta, const flo
   if (p.team(false)) return with_held(act, p.held_vec, [&](auto k) { return k.fwd(p, a, eps, st); });
   dispatch<PartialFwd>(XBAR_ACT_NONE, p.vec, p.lanes, &p, &a, part, st);
   if (launched()) return XBAR_EHIP;
-  hipLaunchKernelGGL(gn_final_fwd_kernel, dim3((unsigned)((batch * groups + 3) / 4)), dim3(256), 0, st, part, p.s, x, eps, mean, invstd);
+  p.finish<false>(part, x, nullptr, eps, mean, invstd, nullptr, st);
   if (launched()) return XBAR_EHIP;
   dispatch<ApplyFwd>(act, p.vec, p.lanes, &p, &a, st);
   return launched();
@@ -730,7 +740,7 @@ int xbar_gn_bwd(const float* x, const float* dy, const float* gamma, const float
   }
   dispatch<PartialBwd>(act, p.vec, p.lanes, &p, &a, part, st);
   if (launched()) return XBAR_EHIP;
-  hipLaunchKernelGGL(gn_final_bwd_kernel, dim3((unsigned)((batch * groups + 3) / 4)), dim3(256), 0, st, part, p.s, gamma, coef);
+  p.finish<true>(part, nullptr, gamma, 0.0f, nullptr, nullptr, coef, st);
   if (launched()) return XBAR_EHIP;
   hipLaunchKernelGGL(gn_parameters_kernel, parameters, dim3(1024), 0, st, part, batch * p.s.chunks, channels, dgamma, dbeta);
   if (launched()) return XBAR_EHIP;

@@ -749,3 +749,10 @@ def test_eager_steps_between_replays(xb):
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     assert all(torch.equal(a.W, b.W) for a, b in zip(eager.layers, mixed_.layers))
+
+
+@pytest.mark.parametrize("shape,groups", [((1, 112, 112, 64), 1), ((2, 70, 61, 50), 1), ((1, 40, 40, 1500), 1), ((3, 50, 51, 96), 2), ((1, 6000, 3), 1), ((1, 90, 91, 5), 1)])
+@pytest.mark.parametrize("kind,skip", [("none", False), ("silu", True)])
+def test_group_norm_of_few_large_groups(xb, shape, groups, kind, skip):
+    """Thousands of partial sums per group, more channels of a group than threads that add them up, and fewer."""
+    gn_check(xb, shape, groups, kind, skip, 3)
