@@ -97,7 +97,8 @@ __device__ __forceinline__ int4 bins_of(const int32_t* rows, int m, int M, int a
   return v;
 }
 
-// Rows of every adapter (bin `adapters`: rows without one), one wave per bin over all rows.
+// Rows of every adapter (bin `adapters`: rows without one), one wave per bin over all rows: this and the placing read rows x adapters numbers
+// (65536 rows, 2048 adapters: 52 + 106 us, from the caches).
 __global__ __launch_bounds__(256) void plan_count_kernel(const int32_t* rows, int M, int adapters, PlanAt p) {
   const int bin = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (bin > adapters) return;
@@ -226,7 +227,8 @@ __global__ __launch_bounds__(256) void plan_place_kernel(const int32_t* rows, in
 }
 
 // The whole plan of a batch of up to 256 rows in one block and launch: a row's place is the number of rows before it in the order (adapter,
-// row), counted from all pairs in LDS.  An adapter has one chunk at most.  (128 rows, 64 adapters: 3 us instead of 11 in three launches.)
+// row), counted from all pairs in LDS.  An adapter has one chunk at most.  (128 rows, 64 adapters: 6.8 us, one row 2.9; 300 rows, 64 adapters
+// in three launches: 3.4 + 4.3 + 5.9.)
 constexpr int kSmallPlan = 256;
 static_assert(kSmallPlan <= 256, "chunk_rows() of the smallest batches");
 __global__ __launch_bounds__(kSmallPlan) void plan_small_kernel(const int32_t* rows, int M, int adapters, PlanAt p) {
@@ -388,7 +390,7 @@ __device__ __forceinline__ void quad_transpose(f4& v0, f4& v1, f4& v2, f4& v3, b
 // lane with its own row: register s holds k = 16 q + 4 s, from both operands, so instruction (s, e) adds up k = 16 q + 4 s + e over the
 // quarters q.  Rows beyond the tile and ranks beyond the last repeat a valid one: their products are not stored.
 // Bound by memory and the issue of loads and products together: 4096 x 4096 floats by rank 32 of 8 adapters 24 us (2.8 TB/s of X; 31 with a lane
-// per row), 128 rows of 57 bfloat16 adapters of rank 16 8.2 us, one row 3.7.
+// per row), 128 rows of 57 bfloat16 adapters of rank 16 8.1 us, one row 3.8.
 template <class T, bool QUADS, int RT>
 __global__ __launch_bounds__(256, RT == 1 ? 4 : RT == 2 ? 3 : RT == 4 ? 2 : 1) void shrink_kernel(PlanAt plan, const float* X, const T* A, float* part, int M, int K, int rank, int adapters,
                                                      int splits, int per_split) {

@@ -2,7 +2,7 @@
 // per sample and group of neighbouring channels -- so that a network runs one request, or trains on small batches.
 //   z = gamma (x - mean) invstd + beta (+ skip),  y = act(z)
 // Evaluated in double precision up to z, rounded once.  HBM-bound elementwise and reduction work: 64 x 56 x 56 x 256 with a skip takes 39 us for the
-// sums (5.3 TB/s), 5 for the statistics and 110 for the values (5.6 TB/s); 64 x 28 x 28 x 512 backward 80 us in one pass (3.9 TB/s).
+// sums (5.3 TB/s), 5 for the statistics and 110 for the values (5.6 TB/s); 64 x 28 x 28 x 512 backward 82 us in one pass (3.8 TB/s).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
